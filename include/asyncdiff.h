@@ -351,6 +351,68 @@ ad_status ad_attention_forward(int dtype, const void* q, const void* k, const vo
 ad_status ad_attention_frames_forward(int dtype, const void* q, const void* k, const void* v, int frames, int positions,
                                       int c, int heads, int ldq, int ldk, int ldv, int ldo, void* out, ad_stream stream);
 
+/* Rotary positions.  The rotated part of a head is its first sum(axis_dims) elements; its pairs are numbered axis after axis.  Pair p turns by
+ * position[axis of p] * f_p: with D = axis_dims[axis] and i = 0 .. D/2 - 1 within the axis, f = base^(-2i/D), changed by `scaling`:
+ *   AD_ROPE_LINEAR  f / factor (positions interpolated);
+ *   AD_ROPE_BASE    base * factor^(D/(D-2)) in place of base;
+ *   AD_ROPE_PARTS   by the turns r = original_len * f / 2 pi of a pair over the original length: f / factor below slow_turns, f above fast_turns,
+ *                   in between (1 - t) f / factor + t f with t = (r - slow_turns) / (fast_turns - slow_turns) (arXiv 2309.00071, Section 3.2).
+ * One axis for a sequence, two or three for the rows and columns (and frames) of an image or a video. */
+#define AD_ROPE_MAX_AXES 3
+typedef enum ad_rope_layout {
+  AD_ROPE_HALF = 0,        /* pair p is elements p and p + (rotated part) / 2 */
+  AD_ROPE_INTERLEAVED = 1  /* pair p is elements 2p and 2p + 1 */
+} ad_rope_layout;
+typedef enum ad_rope_scaling { AD_ROPE_PLAIN = 0, AD_ROPE_LINEAR = 1, AD_ROPE_BASE = 2, AD_ROPE_PARTS = 3 } ad_rope_scaling;
+typedef struct ad_rope_cfg {
+  int layout;                        /* ad_rope_layout */
+  int n_axes;                        /* 1 .. AD_ROPE_MAX_AXES */
+  int axis_dims[AD_ROPE_MAX_AXES];   /* elements of a head each axis turns: even, >= 2; together at most head_dim (and 128) */
+  int scaling;                       /* ad_rope_scaling */
+  double base;                       /* > 1, usually 10000 */
+  double factor;                     /* >= 1, unless AD_ROPE_PLAIN */
+  double original_len, slow_turns, fast_turns;   /* AD_ROPE_PARTS only */
+  double amplitude;                  /* multiplies the rotated elements; 0: 1, with AD_ROPE_PARTS 0.1 ln(factor) + 1 */
+} ad_rope_cfg;
+/* Frequencies of a configuration as the kernels read them (8 bytes a pair): HOST out; the caller copies it to DEVICE memory once.  Returns the
+ * size in bytes through *bytes when out == NULL. */
+ad_status ad_rope_table(const ad_rope_cfg* cfg, void* out, size_t* bytes);
+/* Rotates the heads of q [batch][l][ldq] (heads of head_dim <= 128 elements side by side) and, where kv_heads > 0, of k [batch][l][ldk]; the rest of
+ * a head is copied.  cfg: HOST; table: of the same cfg; positions: int32 [n_axes][l], or with per_sample [batch][n_axes][l], any sign.  q_out [batch][l][ldq_out]
+ * and k_out likewise; q_out may be q and k_out may be k (the same leading dimension), otherwise results must not overlap what is read. */
+ad_status ad_rope_forward(int dtype, const ad_rope_cfg* cfg, const void* table, const int* positions, int per_sample, const void* q, const void* k,
+                          int batch, int l, int heads, int kv_heads, int head_dim, int ldq, int ldk, void* q_out, void* k_out, int ldq_out,
+                          int ldk_out, ad_stream stream);
+/* The same behind a norm over the head_dim elements of every head: AD_NORM_RMS x rsqrt(mean x^2 + eps) gain, AD_NORM_LAYER (x - mean) rsqrt(var + eps) gain
+ * + offset (biased variance).  q_gain, k_gain: fp32 [head_dim], shared by the heads, or NULL (1); q_offset, k_offset: fp32 [head_dim] or NULL (0), AD_NORM_LAYER
+ * only.  eps > 0.  cfg == NULL: the norm alone (table and positions are ignored). */
+typedef enum ad_norm_kind { AD_NORM_RMS = 0, AD_NORM_LAYER = 1 } ad_norm_kind;
+ad_status ad_qk_norm_rope_forward(int dtype, int norm, const ad_rope_cfg* cfg, const void* table, const int* positions, int per_sample, const void* q, const void* k,
+                                  const float* q_gain, const float* k_gain, const float* q_offset, const float* k_offset, float eps, int batch, int l,
+                                  int heads, int kv_heads, int head_dim, int ldq, int ldk, void* q_out, void* k_out, int ldq_out, int ldk_out,
+                                  ad_stream stream);
+
+/* Differential attention (arXiv 2410.05258): with q1 | q2 and k1 | k2 the halves of a head of 2 head_dim columns and v 2 head_dim wide,
+ *   o = (softmax(q1 k1^T / sqrt(head_dim)) - lambda softmax(q2 k2^T / sqrt(head_dim))) v
+ *   out = out_scale * o * rsqrt(mean o^2 + norm_eps) * norm_gain  per head, or out_scale * o where norm_gain is NULL.
+ *   q [batch][l][ldq], out [batch][l][ldo]: `heads` heads of 2 head_dim columns; k [batch][lk][ldk], v [batch][lk][ldv]: `kv_heads` heads, each shared by
+ *   heads / kv_heads query heads that follow each other.  head_dim <= 128, a multiple of 8 (bf16) or 4 (fp32); tensors and rows 16-byte aligned.
+ *   out must not overlap what is read.
+ *   key_lens   int32 [batch] or NULL: sample b has keys 0 .. key_lens[b] - 1 (held to 0 .. lk); what lies behind them does not matter, NaN included;
+ *   causal     query i sees keys 0 .. i + len - l, len the sample's keys (the last query sees them all).  A key that only some rows of the call see
+ *              takes part in the others with weight 0: its values must be finite there;
+ *   lambda     fp32 [heads]; norm_gain fp32 [2 head_dim] or NULL, norm_eps > 0 with it.
+ * A row that sees no key is zero.
+ *   workspace: optional scratch of ad_diff_attention_workspace_bytes(); with it the keys are shared out over workgroups where the rows are few (fixed
+ *   summation order).  Calls that may run at the same time need a workspace each. */
+size_t ad_diff_attention_workspace_bytes(int dtype, int batch, int l, int lk, int heads, int kv_heads, int head_dim);
+ad_status ad_diff_attention_forward(int dtype, const void* q, const void* k, const void* v, int batch, int l, int lk, int heads, int kv_heads,
+                                    int head_dim, int ldq, int ldk, int ldv, int ldo, const int* key_lens, int causal, const float* lambda,
+                                    const float* norm_gain, float norm_eps, float out_scale, void* out, void* workspace, size_t workspace_bytes,
+                                    ad_stream stream);
+/* lambda = exp(q1 . k1) - exp(q2 . k2) + init from a layer's (or head's) learned vectors of n elements; all HOST. */
+ad_status ad_diff_lambda(const float* q1, const float* k1, const float* q2, const float* k2, int n, float init, float* lambda);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,6 +14,10 @@ AD_OK, AD_ERR_INVALID, AD_ERR_NOMEM, AD_ERR_HIP, AD_ERR_DONE, AD_ERR_STATE = ran
 UNIT_KINDS = ["conv_in", "res", "tfm", "down", "up", "out"]
 OUT_ROWMAJOR, OUT_GEGLU, OUT_TRANSPOSED, OUT_TRANSPOSED_F32, OUT_QKV = 0, 1, 2, 3, 4
 
+AD_ROPE_HALF, AD_ROPE_INTERLEAVED = 0, 1
+AD_ROPE_PLAIN, AD_ROPE_LINEAR, AD_ROPE_BASE, AD_ROPE_PARTS = range(4)
+AD_NORM_RMS, AD_NORM_LAYER = 0, 1
+
 lib_path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libasyncdiff.so")
 
 
@@ -71,6 +75,18 @@ class ProfileRec(C.Structure):
     _fields_ = [("kernel", C.c_char * 32), ("flops", C.c_double), ("bytes", C.c_double), ("ms", C.c_float), ("m", C.c_int), ("n", C.c_int), ("k", C.c_int)]
 
 
+class RopeCfg(C.Structure):
+    _fields_ = [("layout", C.c_int), ("n_axes", C.c_int), ("axis_dims", C.c_int * 3), ("scaling", C.c_int), ("base", C.c_double), ("factor", C.c_double),
+                ("original_len", C.c_double), ("slow_turns", C.c_double), ("fast_turns", C.c_double), ("amplitude", C.c_double)]
+
+    @classmethod
+    def make(cls, axis_dims, layout=AD_ROPE_HALF, base=10000.0, scaling=AD_ROPE_PLAIN, factor=1.0, original_len=0.0, slow_turns=1.0, fast_turns=32.0, amplitude=0.0):
+        """axis_dims: elements of a head that each axis of positions turns, one to three of them."""
+        if not 1 <= len(axis_dims) <= 3:
+            raise ValueError("one to three axes")
+        return cls(layout, len(axis_dims), (C.c_int * 3)(*axis_dims), scaling, base, factor, original_len, slow_turns, fast_turns, amplitude)
+
+
 EXPORTS = [
     "ad_create", "ad_destroy", "ad_last_error", "ad_num_units", "ad_get_unit", "ad_get_partition", "ad_component_io",
     "ad_tensor_shape", "ad_num_weights", "ad_get_weight", "ad_device_bytes", "ad_bind_device_memory", "ad_load_weights",
@@ -79,6 +95,7 @@ EXPORTS = [
     "ad_conv_forward", "ad_conv_workspace_bytes", "ad_pack_conv_weight", "ad_groupnorm_scratch_bytes", "ad_groupnorm_forward", "ad_layernorm_forward",
     "ad_attention_forward", "ad_profile_enable", "ad_profile_clear", "ad_profile_count", "ad_profile_get", "ad_profile_ahead", "ad_tune_conv_tile", "ad_precompute_text", "ad_set_graph_mode", "ad_set_edge_mode", "ad_create_with_cuts", "ad_balance_cuts", "ad_tune_conv_order", "ad_create_wrapped", "ad_num_segments",
     "ad_attention_frames_forward", "ad_groupnorm_forward_static", "ad_tune_attention",
+    "ad_rope_table", "ad_rope_forward", "ad_qk_norm_rope_forward", "ad_diff_attention_workspace_bytes", "ad_diff_attention_forward", "ad_diff_lambda",
 ]
 
 
@@ -127,6 +144,12 @@ def _load():
     L.ad_layernorm_forward.argtypes = [ci, vp, ci, ci, vp, vp, cf, vp, vp]
     L.ad_attention_forward.argtypes = [ci, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, ci, vp, vp]
     L.ad_attention_frames_forward.argtypes = [ci, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, vp, vp]
+    L.ad_rope_table.argtypes = [P(RopeCfg), vp, P(sz)]
+    L.ad_rope_forward.argtypes = [ci, P(RopeCfg), vp, vp, ci, vp, vp, ci, ci, ci, ci, ci, ci, ci, vp, vp, ci, ci, vp]
+    L.ad_qk_norm_rope_forward.argtypes = [ci, ci, P(RopeCfg), vp, vp, ci, vp, vp, vp, vp, vp, vp, cf, ci, ci, ci, ci, ci, ci, ci, vp, vp, ci, ci, vp]
+    L.ad_diff_attention_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci, ci]; L.ad_diff_attention_workspace_bytes.restype = sz
+    L.ad_diff_attention_forward.argtypes = [ci, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, ci, vp, ci, vp, vp, cf, cf, vp, vp, sz, vp]
+    L.ad_diff_lambda.argtypes = [vp, vp, vp, vp, ci, cf, P(cf)]
     L.ad_tune_conv_tile.argtypes = [ci]
     L.ad_tune_attention.argtypes = [ci]
     L.ad_precompute_text.argtypes = [vp, vp, vp]
@@ -339,4 +362,13 @@ def pack_conv_weight(dtype, w, geglu=False):
     check(lib.ad_pack_conv_weight(dtype, None, n_out, c_in, k, int(geglu), None, C.byref(nbytes)))
     out = np.zeros(nbytes.value, np.uint8)
     check(lib.ad_pack_conv_weight(dtype, C.c_void_p(w.ctypes.data), n_out, c_in, k, int(geglu), C.c_void_p(out.ctypes.data), C.byref(nbytes)))
+    return out
+
+
+def rope_table(cfg):
+    """The frequencies of a RopeCfg as the kernels read them, a uint8 ndarray (host)."""
+    nbytes = C.c_size_t()
+    check(lib.ad_rope_table(C.byref(cfg), None, C.byref(nbytes)))
+    out = np.zeros(nbytes.value, np.uint8)
+    check(lib.ad_rope_table(C.byref(cfg), C.c_void_p(out.ctypes.data), C.byref(nbytes)))
     return out

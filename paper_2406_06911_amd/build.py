@@ -7,7 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libasyncdiff.so")
-SOURCES = ["ad_host.cpp", "ad_kernels.hip", "ad_rows.hip", "ad_runtime.cpp"]
+SOURCES = ["ad_host.cpp", "ad_kernels.hip", "ad_rows.hip", "ad_rope.hip", "ad_diff_attn.hip", "ad_runtime.cpp"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wno-unused-result", "-Wno-unused-command-line-argument",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

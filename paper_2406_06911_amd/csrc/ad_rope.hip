@@ -1,0 +1,376 @@
+// Rotary positions of queries and keys, by themselves and behind a norm over each head, for gfx950.
+#include "ad_device.h"
+#include "ad_kernels.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+namespace ad {
+
+constexpr int kRopeMaxDim = 128;   // widest head: the limit of the attention kernels too
+
+// =================================================================================================
+// Row (b, i) of q or k is `heads` vectors of d elements.  With a norm, each becomes y = x rsqrt(mean x^2 + eps) gain, or
+// (x - mean) rsqrt(var + eps) gain + offset.  Then pair p of the rotated part, (x_a, x_b), is turned by t = n_p f_p, n_p the row's
+// position on the axis of p:  x_a' = A (x_a cos t - x_b sin t),  x_b' = A (x_b cos t + x_a sin t).
+//
+// The angle: positions are whole numbers, so whole turns may be dropped from the frequency and from the product.  f / 2 pi is held as a
+// fraction of a turn in 64 bits, the product with the position is taken modulo one turn in whole numbers, and its upper 32 bits are the
+// phase: exact to 2^-32 turn plus position * 2^-64, however far the position is (an fp32 product at position 10^6 is off by 0.06 rad).
+// v_sin_f32 / v_cos_f32 take turns; over one turn they are off by at most 1.3e-7 (rms 3.5e-8, measured at 2^20 phases), less than
+// an fp32 angle's own rounding, so fp32 tensors use them as well.
+//
+// A head is shared out over a power of two of lanes, each with two accesses of VN elements (up to 16 bytes each): the two sides of VN pairs
+// where the pairs lie half the rotated part apart, VN pairs in a row where they are neighbours; the part that is not rotated lies behind.
+// The norm's sums go over those lanes.  Such a group of lanes walks `slots`-th heads of its row and forms its angles once for all of them.
+// Bound by memory: every element is read once and written once; a lane may write where it has read, so q_out may be q.
+// =================================================================================================
+struct RopeSide {
+  const void* src; void* dst;
+  const float *gain, *offset;
+  int heads, ld, ldo;
+  int log_slots;                 // 2^log_slots groups of lanes share a row
+  unsigned blocks;
+};
+struct RopeParams {
+  RopeSide side[2];              // q, k
+  const unsigned long long* table;
+  const int* positions;
+  long long sample_positions;    // positions of a sample, 0: shared
+  unsigned rows, l;
+  FastDiv div_l;
+  int d, pairs, n_axes, axis_end[AD_ROPE_MAX_AXES];   // last pair of an axis + 1
+  int units, log_lanes;          // lanes' shares of a head, lanes of a head
+  float eps, amplitude, inv_d;
+};
+
+template <typename T, int VN> struct alignas(VN * sizeof(T)) Access { T v[VN]; };
+
+enum { ROPE_NO_NORM = -1 };
+
+// sum over the 2^log_lanes neighbouring lanes of a head
+__device__ __forceinline__ float head_sum(float v, int log_lanes) {
+  if (log_lanes > 0) v += dpp_f<0xB1>(v);
+  if (log_lanes > 1) v += dpp_f<0x4E>(v);
+  if (log_lanes > 2) v += dpp_f<0x141>(v);
+  if (log_lanes > 3) v += dpp_f<0x140>(v);
+  if (log_lanes > 4) v += __shfl_xor(v, 16, 64);
+  if (log_lanes > 5) v += __shfl_xor(v, 32, 64);
+  return v;
+}
+
+template <typename T, int VN, int LAYOUT, int NORM>
+__global__ __launch_bounds__(256) void k_rope(RopeParams p) {
+  typedef Access<T, VN> V;
+  const bool is_k = blockIdx.x >= p.side[0].blocks;
+  const RopeSide& s = p.side[is_k];
+  const unsigned block = blockIdx.x - (is_k ? p.side[0].blocks : 0u);
+  const int unit = threadIdx.x & ((1 << p.log_lanes) - 1);
+  const unsigned group = threadIdx.x >> p.log_lanes;
+  const int log_groups = 8 - p.log_lanes;
+  const unsigned row = (block << (log_groups - s.log_slots)) + (group >> s.log_slots);
+  const int slot = group & ((1 << s.log_slots) - 1);
+  const bool live = row < p.rows && unit < p.units;
+
+  // where this lane's two accesses lie in a head
+  const int turning = p.pairs / VN;              // lanes with rotated pairs
+  const bool turns = unit < turning;
+  int at_a, at_b;
+  if (turns) {
+    at_a = LAYOUT == AD_ROPE_HALF ? unit * VN : 2 * unit * VN;
+    at_b = at_a + (LAYOUT == AD_ROPE_HALF ? p.pairs : VN);
+  } else {
+    at_a = 2 * p.pairs + 2 * (unit - turning) * VN;
+    at_b = at_a + VN;
+  }
+  const bool has_a = live && at_a < p.d, has_b = live && at_b < p.d;
+
+  const T* const src = (const T*)s.src + (size_t)(live ? row : 0) * s.ld;
+  T* const dst = (T*)s.dst + (size_t)(live ? row : 0) * s.ldo;
+  constexpr int UN = 4;                          // heads in flight
+  V a[UN], b[UN];
+  const int step = 1 << s.log_slots;
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int h = h0 + u * step;
+      const bool on = h < s.heads;
+      if (on && has_a) a[u] = *(const V*)(src + (size_t)h * p.d + at_a);
+      if (on && has_b) b[u] = *(const V*)(src + (size_t)h * p.d + at_b);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < UN; ++u)
+#pragma unroll
+    for (int e = 0; e < VN; ++e) { a[u].v[e] = from_f<T>(0.f); b[u].v[e] = from_f<T>(0.f); }
+  fetch(slot);
+
+  float co[VN], si[VN];
+#pragma unroll
+  for (int e = 0; e < VN; ++e) { co[e] = 1.f; si[e] = 0.f; }
+  if (live && turns) {
+    const unsigned sample = fast_div(row, p.div_l);
+    const int* const pos = p.positions + (size_t)sample * p.sample_positions + (row - sample * p.l);
+    int n[AD_ROPE_MAX_AXES];
+#pragma unroll
+    for (int x = 0; x < AD_ROPE_MAX_AXES; ++x) n[x] = x < p.n_axes ? pos[(size_t)x * p.l] : 0;
+#pragma unroll
+    for (int e = 0; e < VN; ++e) {
+      const int pair = unit * VN + e;
+      const unsigned long long f = p.table[pair];
+      const int at = pair < p.axis_end[0] ? n[0] : (pair < p.axis_end[1] ? n[1] : n[2]);
+      const unsigned phase = (unsigned)(((unsigned long long)(long long)at * f) >> 32);
+      const float turn = (float)(int)phase * 0x1p-32f;
+      co[e] = __builtin_amdgcn_cosf(turn) * p.amplitude;
+      si[e] = __builtin_amdgcn_sinf(turn) * p.amplitude;
+    }
+  }
+  float ga[VN], gb[VN], oa[VN], ob[VN];
+  if constexpr (NORM != ROPE_NO_NORM) {
+#pragma unroll
+    for (int e = 0; e < VN; ++e) {
+      ga[e] = s.gain && has_a ? s.gain[at_a + e] : 1.f;
+      gb[e] = s.gain && has_b ? s.gain[at_b + e] : 1.f;
+      oa[e] = NORM == AD_NORM_LAYER && s.offset && has_a ? s.offset[at_a + e] : 0.f;
+      ob[e] = NORM == AD_NORM_LAYER && s.offset && has_b ? s.offset[at_b + e] : 0.f;
+    }
+  }
+
+  for (int h0 = slot; h0 < s.heads; h0 += UN * step) {
+    if (h0 > slot) fetch(h0);
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int h = h0 + u * step;
+      if (h >= s.heads) break;
+      float x[VN], y[VN];
+#pragma unroll
+      for (int e = 0; e < VN; ++e) { x[e] = to_f(a[u].v[e]); y[e] = to_f(b[u].v[e]); }
+      if constexpr (NORM != ROPE_NO_NORM) {
+        if constexpr (NORM == AD_NORM_LAYER) {
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < VN; ++e) sum += x[e] + y[e];
+          const float mean = head_sum(sum, p.log_lanes) * p.inv_d;
+#pragma unroll
+          for (int e = 0; e < VN; ++e) {
+            x[e] = has_a ? x[e] - mean : 0.f;
+            y[e] = has_b ? y[e] - mean : 0.f;
+          }
+        }
+        float sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < VN; ++e) sq = fmaf(x[e], x[e], fmaf(y[e], y[e], sq));
+        const float r = rsqrtf(head_sum(sq, p.log_lanes) * p.inv_d + p.eps);
+#pragma unroll
+        for (int e = 0; e < VN; ++e) {
+          x[e] = fmaf(x[e] * r, ga[e], oa[e]);
+          y[e] = fmaf(y[e] * r, gb[e], ob[e]);
+        }
+      }
+      if (turns) {
+        if constexpr (LAYOUT == AD_ROPE_HALF) {
+#pragma unroll
+          for (int e = 0; e < VN; ++e) {
+            const float xe = x[e], ye = y[e];
+            x[e] = fmaf(xe, co[e], -(ye * si[e]));
+            y[e] = fmaf(ye, co[e], xe * si[e]);
+          }
+        } else if constexpr (VN == 1) {
+          const float xe = x[0], ye = y[0];
+          x[0] = fmaf(xe, co[0], -(ye * si[0]));
+          y[0] = fmaf(ye, co[0], xe * si[0]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VN; e += 2) {
+            const float x0 = x[e], x1 = x[e + 1], y0 = y[e], y1 = y[e + 1];
+            x[e] = fmaf(x0, co[e / 2], -(x1 * si[e / 2]));
+            x[e + 1] = fmaf(x1, co[e / 2], x0 * si[e / 2]);
+            y[e] = fmaf(y0, co[(VN + e) / 2], -(y1 * si[(VN + e) / 2]));
+            y[e + 1] = fmaf(y1, co[(VN + e) / 2], y0 * si[(VN + e) / 2]);
+          }
+        }
+      }
+      V wa, wb;
+#pragma unroll
+      for (int e = 0; e < VN; ++e) { wa.v[e] = from_f<T>(x[e]); wb.v[e] = from_f<T>(y[e]); }
+      if (has_a) *(V*)(dst + (size_t)h * p.d + at_a) = wa;
+      if (has_b) *(V*)(dst + (size_t)h * p.d + at_b) = wb;
+    }
+  }
+}
+
+static ad_status check_rope(const ad_rope_cfg* c, const char* who) {
+  if (!c) AD_FAIL(AD_ERR_INVALID, "%s: null configuration", who);
+  if (c->layout != AD_ROPE_HALF && c->layout != AD_ROPE_INTERLEAVED) AD_FAIL(AD_ERR_INVALID, "%s: bad layout", who);
+  if (c->n_axes < 1 || c->n_axes > AD_ROPE_MAX_AXES) AD_FAIL(AD_ERR_INVALID, "%s: 1..%d axes", who, AD_ROPE_MAX_AXES);
+  int sum = 0;
+  for (int a = 0; a < c->n_axes; ++a) {
+    if (c->axis_dims[a] < 2 || c->axis_dims[a] % 2 || c->axis_dims[a] > kRopeMaxDim) AD_FAIL(AD_ERR_INVALID, "%s: an axis turns an even number of elements, 2..%d", who, kRopeMaxDim);
+    sum += c->axis_dims[a];
+  }
+  if (sum > kRopeMaxDim) AD_FAIL(AD_ERR_INVALID, "%s: the axes turn %d elements, at most %d", who, sum, kRopeMaxDim);
+  if (!(c->base > 1.0) || !std::isfinite(c->base)) AD_FAIL(AD_ERR_INVALID, "%s: base must be above 1", who);
+  if (!(c->amplitude >= 0.0) || !std::isfinite(c->amplitude)) AD_FAIL(AD_ERR_INVALID, "%s: bad amplitude", who);
+  if (c->scaling < AD_ROPE_PLAIN || c->scaling > AD_ROPE_PARTS) AD_FAIL(AD_ERR_INVALID, "%s: bad scaling", who);
+  if (c->scaling != AD_ROPE_PLAIN && (!(c->factor >= 1.0) || !std::isfinite(c->factor))) AD_FAIL(AD_ERR_INVALID, "%s: the scaling's factor must be at least 1", who);
+  if (c->scaling == AD_ROPE_PARTS && (!(c->original_len > 0.0) || !std::isfinite(c->original_len) || !(c->slow_turns >= 0.0) || !(c->fast_turns > c->slow_turns) || !std::isfinite(c->fast_turns)))
+    AD_FAIL(AD_ERR_INVALID, "%s: scaling by parts needs the original length and 0 <= slow_turns < fast_turns", who);
+  return AD_OK;
+}
+
+static double rope_amplitude(const ad_rope_cfg& c) {
+  if (c.amplitude > 0.0) return c.amplitude;
+  return c.scaling == AD_ROPE_PARTS ? 0.1 * std::log(c.factor) + 1.0 : 1.0;
+}
+
+// turns a position, modulo one, as a fraction of 2^64
+static unsigned long long turn_fraction(double radians) {
+  long double t = (long double)radians / 6.283185307179586476925286766559L;
+  t -= floorl(t);
+  const long double scaled = roundl(ldexpl(t, 64));
+  return scaled >= 18446744073709551616.0L ? 0ull : (unsigned long long)scaled;
+}
+
+static ad_status launch_rope(const char* name, int dtype, int norm, const ad_rope_cfg* cfg, const void* table, const int* positions, int per_sample, const void* q,
+                             const void* k, const float* q_gain, const float* k_gain, const float* q_offset, const float* k_offset, float eps, int batch,
+                             int l, int heads, int kv_heads, int d, int ldq, int ldk, void* q_out, void* k_out, int ldq_out, int ldk_out, hipStream_t s) {
+  if (dtype != AD_BF16 && dtype != AD_F32) AD_FAIL(AD_ERR_INVALID, "%s: bad dtype", name);
+  if (!q || !q_out || (kv_heads > 0 && (!k || !k_out))) AD_FAIL(AD_ERR_INVALID, "%s: null pointer", name);
+  if (batch < 1 || l < 1 || heads < 1 || kv_heads < 0 || d < 1 || d > kRopeMaxDim || (long long)batch * l > 0x7fffffffLL)
+    AD_FAIL(AD_ERR_INVALID, "%s: bad shape (head_dim 1..%d)", name, kRopeMaxDim);
+  if ((long long)heads * d > 0x7fffffffLL || (long long)kv_heads * d > 0x7fffffffLL) AD_FAIL(AD_ERR_INVALID, "%s: too many heads", name);
+  if (ldq < heads * d || ldq_out < heads * d || (kv_heads > 0 && (ldk < kv_heads * d || ldk_out < kv_heads * d))) AD_FAIL(AD_ERR_INVALID, "%s: bad leading dimension", name);
+  if ((q == q_out && ldq != ldq_out) || (kv_heads > 0 && k == k_out && ldk != ldk_out)) AD_FAIL(AD_ERR_INVALID, "%s: in place, both leading dimensions are the same", name);
+  if (kv_heads > 0 && q_out == k_out) AD_FAIL(AD_ERR_INVALID, "%s: q_out and k_out are the same", name);
+  const size_t es = esize(dtype);
+  uintptr_t all = (uintptr_t)q | (uintptr_t)q_out | (kv_heads > 0 ? (uintptr_t)k | (uintptr_t)k_out : 0);
+  if (all % es) AD_FAIL(AD_ERR_INVALID, "%s: a tensor is not aligned to its type", name);
+  RopeParams p{};
+  int pairs = 0;
+  if (cfg) {
+    const ad_status st = check_rope(cfg, name);
+    if (st != AD_OK) return st;
+    if (!table || !positions) AD_FAIL(AD_ERR_INVALID, "%s: null table or positions", name);
+    if ((uintptr_t)table % 8 || (uintptr_t)positions % 4) AD_FAIL(AD_ERR_INVALID, "%s: table or positions not aligned to their type", name);
+    for (int a = 0; a < AD_ROPE_MAX_AXES; ++a) {
+      if (a < cfg->n_axes) pairs += cfg->axis_dims[a] / 2;
+      p.axis_end[a] = pairs;
+    }
+    if (2 * pairs > d) AD_FAIL(AD_ERR_INVALID, "%s: the axes turn %d elements of a head of %d", name, 2 * pairs, d);
+    p.n_axes = cfg->n_axes;
+    p.amplitude = (float)rope_amplitude(*cfg);
+  }
+  if (norm != ROPE_NO_NORM) {
+    if (norm != AD_NORM_RMS && norm != AD_NORM_LAYER) AD_FAIL(AD_ERR_INVALID, "%s: bad norm", name);
+    if (!(eps > 0.f) || !std::isfinite(eps)) AD_FAIL(AD_ERR_INVALID, "%s: eps must be above 0", name);
+    if (norm == AD_NORM_RMS && (q_offset || k_offset)) AD_FAIL(AD_ERR_INVALID, "%s: an RMS norm has no offset", name);
+    if (((uintptr_t)q_gain | (uintptr_t)k_gain | (uintptr_t)q_offset | (uintptr_t)k_offset) % 4) AD_FAIL(AD_ERR_INVALID, "%s: gain or offset not aligned to its type", name);
+  }
+  // the widest access that pairs, heads, rows and addresses allow
+  int vn = 16 / (int)es;
+  const int lds = ldq | ldq_out | (kv_heads > 0 ? ldk | ldk_out : 0);
+  while (vn > 1 && (pairs % vn || d % vn || lds % vn || all % (vn * es))) vn >>= 1;
+  p.units = pairs / vn + (d - 2 * pairs + 2 * vn - 1) / (2 * vn);
+  while ((1 << p.log_lanes) < p.units) ++p.log_lanes;
+  p.rows = (unsigned)((long long)batch * l);
+  p.l = (unsigned)l;
+  p.div_l = make_fastdiv(p.l);
+  p.d = d; p.pairs = pairs;
+  p.table = (const unsigned long long*)table;
+  p.positions = positions;
+  p.sample_positions = per_sample ? (long long)p.n_axes * l : 0;
+  p.eps = eps; p.inv_d = 1.f / (float)d;
+  p.side[0] = RopeSide{q, q_out, q_gain, q_offset, heads, ldq, ldq_out, 0, 0};
+  p.side[1] = RopeSide{k, k_out, k_gain, k_offset, kv_heads, ldk, ldk_out, 0, 0};
+  const int log_groups = 8 - p.log_lanes;
+  for (auto& side : p.side) {
+    if (side.heads == 0) continue;
+    // a group of lanes takes four heads of a row; where that leaves the chip idle, fewer
+    while ((4 << side.log_slots) < side.heads && side.log_slots < log_groups) ++side.log_slots;
+    while ((1 << side.log_slots) < side.heads && side.log_slots < log_groups && ((unsigned long long)p.rows << (side.log_slots + p.log_lanes)) < 256 * 1024) ++side.log_slots;
+    const int rows_a_block = 1 << (log_groups - side.log_slots);
+    side.blocks = (p.rows + rows_a_block - 1) / rows_a_block;
+  }
+  const double elements = (double)p.rows * (heads + kv_heads) * d;
+  ProfLaunch pl(norm == ROPE_NO_NORM ? "rope" : "qk_norm_rope", 0, 2.0 * es * elements, s);
+  const dim3 grid(p.side[0].blocks + p.side[1].blocks);
+  const int layout = cfg ? cfg->layout : AD_ROPE_HALF;
+#define AD_ROPE_RUN(T_, VN_, LAYOUT_, NORM_) hipLaunchKernelGGL((k_rope<T_, VN_, LAYOUT_, NORM_>), grid, dim3(256), 0, s, p)
+#define AD_ROPE_NORM(T_, VN_, LAYOUT_)                                                \
+  if (norm == ROPE_NO_NORM) AD_ROPE_RUN(T_, VN_, LAYOUT_, ROPE_NO_NORM);              \
+  else if (norm == AD_NORM_RMS) AD_ROPE_RUN(T_, VN_, LAYOUT_, AD_NORM_RMS);           \
+  else AD_ROPE_RUN(T_, VN_, LAYOUT_, AD_NORM_LAYER)
+#define AD_ROPE_LAYOUT(T_, VN_)                                                       \
+  if (layout == AD_ROPE_HALF) { AD_ROPE_NORM(T_, VN_, AD_ROPE_HALF); }                \
+  else { AD_ROPE_NORM(T_, VN_, AD_ROPE_INTERLEAVED); }
+  if (dtype == AD_BF16) {
+    if (vn == 8) { AD_ROPE_LAYOUT(bf16, 8) }
+    else if (vn == 4) { AD_ROPE_LAYOUT(bf16, 4) }
+    else if (vn == 2) { AD_ROPE_LAYOUT(bf16, 2) }
+    else { AD_ROPE_LAYOUT(bf16, 1) }
+  } else {
+    if (vn == 4) { AD_ROPE_LAYOUT(float, 4) }
+    else if (vn == 2) { AD_ROPE_LAYOUT(float, 2) }
+    else { AD_ROPE_LAYOUT(float, 1) }
+  }
+#undef AD_ROPE_LAYOUT
+#undef AD_ROPE_NORM
+#undef AD_ROPE_RUN
+  AD_HIP(hipGetLastError());
+  return AD_OK;
+}
+
+}  // namespace ad
+
+using namespace ad;
+
+extern "C" {
+
+ad_status ad_rope_table(const ad_rope_cfg* cfg, void* out, size_t* bytes) {
+  const ad_status st = check_rope(cfg, "rope table");
+  if (st != AD_OK) return st;
+  int pairs = 0;
+  for (int a = 0; a < cfg->n_axes; ++a) pairs += cfg->axis_dims[a] / 2;
+  if (bytes) *bytes = (size_t)pairs * 8;
+  else if (!out) AD_FAIL(AD_ERR_INVALID, "rope table: null pointer");
+  if (!out) return AD_OK;
+  char* to = (char*)out;
+  for (int a = 0; a < cfg->n_axes; ++a) {
+    const int dim = cfg->axis_dims[a];
+    double base = cfg->base;
+    if (cfg->scaling == AD_ROPE_BASE && dim > 2) base *= std::pow(cfg->factor, (double)dim / (dim - 2));
+    for (int i = 0; i < dim / 2; ++i) {
+      double f = std::pow(base, -2.0 * i / dim);
+      if (cfg->scaling == AD_ROPE_LINEAR) f /= cfg->factor;
+      if (cfg->scaling == AD_ROPE_PARTS) {
+        const double turns = cfg->original_len * f / 6.283185307179586476925286766559;
+        const double keep = std::min(1.0, std::max(0.0, (turns - cfg->slow_turns) / (cfg->fast_turns - cfg->slow_turns)));
+        f = f / cfg->factor * (1.0 - keep) + f * keep;
+      }
+      const unsigned long long t = turn_fraction(f);
+      std::memcpy(to, &t, 8);
+      to += 8;
+    }
+  }
+  return AD_OK;
+}
+
+ad_status ad_rope_forward(int dtype, const ad_rope_cfg* cfg, const void* table, const int* positions, int per_sample, const void* q, const void* k,
+                          int batch, int l, int heads, int kv_heads, int head_dim, int ldq, int ldk, void* q_out, void* k_out, int ldq_out,
+                          int ldk_out, ad_stream stream) {
+  if (!cfg) AD_FAIL(AD_ERR_INVALID, "rope: null configuration");
+  return launch_rope("rope", dtype, ROPE_NO_NORM, cfg, table, positions, per_sample, q, k, nullptr, nullptr, nullptr, nullptr, 0.f, batch, l, heads, kv_heads,
+                     head_dim, ldq, ldk, q_out, k_out, ldq_out, ldk_out, (hipStream_t)stream);
+}
+
+ad_status ad_qk_norm_rope_forward(int dtype, int norm, const ad_rope_cfg* cfg, const void* table, const int* positions, int per_sample, const void* q, const void* k,
+                                  const float* q_gain, const float* k_gain, const float* q_offset, const float* k_offset, float eps, int batch, int l,
+                                  int heads, int kv_heads, int head_dim, int ldq, int ldk, void* q_out, void* k_out, int ldq_out, int ldk_out,
+                                  ad_stream stream) {
+  if (norm != AD_NORM_RMS && norm != AD_NORM_LAYER) AD_FAIL(AD_ERR_INVALID, "qk norm: bad norm");
+  return launch_rope("qk norm", dtype, norm, cfg, table, positions, per_sample, q, k, q_gain, k_gain, q_offset, k_offset, eps, batch, l, heads, kv_heads,
+                     head_dim, ldq, ldk, q_out, k_out, ldq_out, ldk_out, (hipStream_t)stream);
+}
+
+}  // extern "C"
