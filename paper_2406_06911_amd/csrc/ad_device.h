@@ -105,6 +105,28 @@ __device__ __forceinline__ V buffer_load16(__amdgpu_buffer_rsrc_t r, unsigned vo
   return __builtin_bit_cast(V, raw);
 }
 
+// Loads of the load unit into LDS: 16 bytes a lane, written at lds_addr + lane * 16.  From inline assembly, so that a loop can wait for exactly the
+// tile it is about to use.
+__device__ __forceinline__ void dma_load16(u32x4 rsrc, unsigned voffset, unsigned soffset, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :: "s"(lds_addr), "v"(voffset), "s"(rsrc), "s"(soffset) : "memory");
+}
+__device__ __forceinline__ u32x4 make_rsrc_words(const void* base, unsigned bytes) {
+  const unsigned long long a = (unsigned long long)base;
+  return u32x4{(unsigned)a, (unsigned)(a >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+// waits until at most n of this wavefront's vector-memory operations are outstanding (n < 64)
+template <int N> __device__ __forceinline__ void wait_vmcnt() {
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+
+// the value of the lane 32 away (low: this lane is one of the first 32)
+__device__ __forceinline__ float other_half(float x, bool low) {
+  const unsigned u = __float_as_uint(x);
+  auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(low ? r[1] : r[0]);
+}
+
 template <typename T> struct Vec4;
 template <> struct Vec4<bf16> { typedef bf16x4 type; };
 template <> struct Vec4<float> { typedef f32x4 type; };

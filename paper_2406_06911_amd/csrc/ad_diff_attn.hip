@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 namespace ad {
 
@@ -200,6 +201,281 @@ __global__ __launch_bounds__(512) void k_diff_generic(DiffParams p) {
   }
 }
 
+// =================================================================================================
+// bf16.  Tiles of 64 keys and their values are brought into LDS by the load unit, two stages.  A tile of k and one of v have the same shape: 64 rows of the
+// head's 2 d columns (k1 | k2), on a pitch of 128, 256 or 512 bytes; columns behind 2 d and keys behind the sample's length read as zeros.  Scores are
+// computed transposed (S^T = K Q^T, a lane owns a row), so the probabilities are the B operand of O^T += V^T P^T as they stand; V^T fragments are read from
+// the row-major tile by the transposing LDS read, four keys of a column at a time.
+//
+// The exponential's reference need not be the running maximum: any value near it gives the same quotient.  It is the exact maximum of the first 32 keys
+// that a row sees, and is raised (and what has been summed rescaled) when a block's sum of weights reaches 2^24, so the steady state computes no
+// maximum.  A row sees a prefix of its keys, so where it sees any of a share, it sees the first.
+//
+// A wavefront owns 32 rows and both maps: a fragment of v serves two products.  FEW: for few rows, a workgroup takes 32 rows, and its four wavefronts take a
+// map and every other block of 32 keys each; their sums meet in LDS.
+//
+// Probabilities are rounded to bf16 for the product with v, scores, sums and references are fp32; q is not scaled in front of the product (a rounding less).
+// =================================================================================================
+constexpr int diff_pitch(int nc) { return nc <= 2 ? 128 : nc <= 4 ? 256 : 512; }
+constexpr float kDiffBig = 16777216.f;
+
+template <int NC, bool FEW>
+__global__ __launch_bounds__(256, NC <= 2 ? 3 : NC <= 4 ? 2 : 1) void k_diff_mfma(DiffParams p) {
+  constexpr int PITCH = diff_pitch(NC), CPR = PITCH / 16, TILE = 64 * PITCH, STAGE = 2 * TILE, LPT = TILE / 4096;
+  constexpr int MAPS = FEW ? 1 : 2, ROWS = FEW ? 32 : 128;
+  extern __shared__ __attribute__((aligned(128))) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const bool low = half == 0;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int map0 = FEW ? wave & 1 : 0, my_block = wave >> 1;
+  const unsigned vid = xcd_remap(blockIdx.x, gridDim.x);
+  const unsigned bt = fast_div(vid, p.div_splits), split = vid - bt * p.splits;
+  const unsigned bh = fast_div(bt, p.div_tiles), tile = bt - bh * p.tiles;
+  const unsigned b = fast_div(bh, p.div_kv), hk = bh - b * p.kv_heads;
+  const int d = p.d, w = 2 * d, d8 = d >> 3;
+  const int len = __builtin_amdgcn_readfirstlane(p.key_lens ? min(max(p.key_lens[b], 0), p.lk) : p.lk);
+  auto limit_of = [&](int row) {
+    return p.causal ? min(max((int)fast_div((unsigned)min(row, p.rows - 1), p.div_group) + len - p.l + 1, 0), len) : len;
+  };
+  const int row0 = tile * ROWS + (FEW ? 0 : wave * 32), row = row0 + l32;
+  const int rowc = min(row, p.rows - 1);                       // rows behind the last repeat it, and are not stored
+  const int i = (int)fast_div((unsigned)rowc, p.div_group), hg = rowc - i * p.group;
+  const int limit = limit_of(row), lim_first = limit_of(row0), lim_last = limit_of(row0 + 31);
+  const int from = split * p.split_keys, to = min(from + p.split_keys, limit_of(tile * ROWS + ROWS - 1));
+  const int ntiles = to > from ? (to - from + 63) >> 6 : 0;
+
+  // ---- tile loads
+  const bf16* const kbase = (const bf16*)p.k + (size_t)b * p.lk * p.ldk + (size_t)hk * w;
+  const bf16* const vbase = (const bf16*)p.v + (size_t)b * p.lk * p.ldv + (size_t)hk * w;
+  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
+  auto issue = [&](int t, int stage) {
+    const int key0 = from + 64 * t, n = min(64, len - key0);
+    const u32x4 rk = make_rsrc_words(kbase + (size_t)key0 * p.ldk, (unsigned)((n - 1) * p.ldk + w) * 2u);
+    const u32x4 rv = make_rsrc_words(vbase + (size_t)key0 * p.ldv, (unsigned)((n - 1) * p.ldv + w) * 2u);
+    const unsigned at = lds_base + stage * STAGE + wave * 1024u;
+#pragma unroll
+    for (int x = 0; x < LPT; ++x) {
+      const int id = (x * 4 + wave) * 64 + lane, r = id / CPR, pos = id % CPR;
+      const int ck = pos ^ (PITCH == 128 ? (r >> 1) & 7 : r & 15), cv = pos ^ (PITCH == 128 ? (r << 1) & 4 : (r & 3) << 2);
+      dma_load16(rk, ck * 8 < w ? (unsigned)(r * p.ldk) * 2u + ck * 16u : kOob, 0u, at + x * 4096u);
+      dma_load16(rv, cv * 8 < w ? (unsigned)(r * p.ldv) * 2u + cv * 16u : kOob, 0u, at + TILE + x * 4096u);
+    }
+  };
+  if (ntiles > 0) issue(0, 0);
+
+  // ---- queries: B operand of the score product
+  const bf16* const qrow = (const bf16*)p.q + ((size_t)b * p.l + i) * p.ldq + (size_t)(hk * p.group + hg) * w;
+  bf16x8 qf[MAPS][NC];
+#pragma unroll
+  for (int m = 0; m < MAPS; ++m)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qf[m][c][e] = (bf16)0.f;
+      if (16 * c + 8 * half < d) qf[m][c] = *(const bf16x8*)(qrow + (map0 + m) * d + 16 * c + 8 * half);
+    }
+  f32x16 o[MAPS][NC];
+  float m_ref[MAPS], neg[MAPS], l_run[MAPS];
+#pragma unroll
+  for (int m = 0; m < MAPS; ++m) {
+    m_ref[m] = -INFINITY; neg[m] = 0.f; l_run[m] = 0.f;
+#pragma unroll
+    for (int t = 0; t < NC; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[m][t][r] = 0.f;
+  }
+  // fragment offsets in a tile: K row l32, 16-byte chunk map * d / 8 + 2 c + half at its swizzled place
+  const int k_swz = PITCH == 128 ? (l32 >> 1) & 7 : l32 & 15;
+  // V: the 16 lanes of a group read four keys' 16 columns; lane x of a group addresses key x / 4, columns 4 (x % 4)
+  const int x16 = lane & 15, v_row = 4 * half + (x16 >> 2), v_chunk = 2 * ((lane >> 4) & 1) + ((x16 & 3) >> 1);
+  const int v_swz = PITCH == 128 ? (v_row << 1) & 4 : (v_row & 3) << 2;
+  const int v_base = v_row * PITCH + 8 * (x16 & 1);
+
+  auto block = [&](const char* Ks, int j, int kb, bool masked) {
+    const char* Vs = Ks + TILE;
+    f32x16 s[MAPS];
+#pragma unroll
+    for (int m = 0; m < MAPS; ++m) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[m][r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const bf16x8 kf = *(const bf16x8*)(Ks + (j * 32 + l32) * PITCH + ((((map0 + m) * d8 + 2 * c + half) ^ k_swz) << 4));
+        s[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[m][c], s[m], 0, 0, 0);
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int m = 0; m < MAPS; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (kb + 8 * (r >> 2) + 4 * half + (r & 3) >= limit) s[m][r] = -INFINITY;
+    }
+    bf16x8 pb[MAPS][2];
+    auto probs = [&](int m) {
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[m][r], p.scale_log2, neg[m]));
+        sum += e;
+        pb[m][r >> 3][r & 7] = (bf16)e;
+      }
+      return sum;
+    };
+    float sum[MAPS];
+    bool redo[MAPS], any = false;
+#pragma unroll
+    for (int m = 0; m < MAPS; ++m) {
+      sum[m] = probs(m);
+      redo[m] = !(sum[m] < kDiffBig) || m_ref[m] == -INFINITY;
+      any |= redo[m];
+    }
+    if (__builtin_amdgcn_ballot_w64(any) != 0) {
+#pragma unroll
+      for (int m = 0; m < MAPS; ++m) {
+        // only rows that asked for it (either half) move: what a row gives does not depend on the rows beside it
+        const float mine = redo[m] ? 1.f : 0.f;
+        const bool move = mine + other_half(mine, low) != 0.f;
+        float a = s[m][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) a = fmaxf(a, s[m][r]);
+        a = fmaxf(a, other_half(a, low)) * p.scale_log2;
+        const float up = move ? fmaxf(m_ref[m], a) : m_ref[m];
+        const float keep = !move || m_ref[m] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_ref[m] - up);
+        m_ref[m] = up;
+        neg[m] = up == -INFINITY ? 0.f : -up;
+        l_run[m] *= keep;
+#pragma unroll
+        for (int t = 0; t < NC; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[m][t][r] *= keep;
+        sum[m] = probs(m);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < MAPS; ++m) l_run[m] += sum[m];
+#pragma unroll
+    for (int t = 0; t < NC; ++t)
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const char* at = Vs + (j * 32 + 16 * s2) * PITCH + v_base + (((4 * t + v_chunk) ^ v_swz) << 4);
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+        const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * PITCH));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int m = 0; m < MAPS; ++m) o[m][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[m][s2], o[m][t], 0, 0, 0);
+      }
+  };
+
+  for (int t = 0; t < ntiles; ++t) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1);
+    const char* const Ks = lds + (t & 1) * STAGE;
+#pragma unroll 1
+    for (int j = FEW ? my_block : 0; j < (FEW ? my_block + 1 : 2); ++j) {
+      const int kb = from + 64 * t + 32 * j;
+      if (kb < lim_last) block(Ks, j, kb, kb + 32 > lim_first);
+    }
+  }
+
+  float l_tot[MAPS];
+#pragma unroll
+  for (int m = 0; m < MAPS; ++m) l_tot[m] = l_run[m] + other_half(l_run[m], low);
+  float* const hand = (float*)lds;
+  constexpr int HAND = (16 * NC + 2) * 64;                     // a wavefront's sums, a register of all lanes at a time
+  if constexpr (FEW) {
+    // the second block's wavefronts hand theirs to the first's
+    __syncthreads();
+    float* const at = hand + map0 * HAND + lane;
+    if (my_block == 1) {
+#pragma unroll
+      for (int t = 0; t < NC; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) at[(16 * t + r) * 64] = o[0][t][r];
+      at[16 * NC * 64] = m_ref[0];
+      at[(16 * NC + 1) * 64] = l_tot[0];
+    }
+    __syncthreads();
+    if (my_block == 0) {
+      const float other = at[16 * NC * 64], up = fmaxf(m_ref[0], other), ref = up == -INFINITY ? 0.f : up;
+      const float f0 = __builtin_amdgcn_exp2f(m_ref[0] - ref), f1 = __builtin_amdgcn_exp2f(other - ref);
+      m_ref[0] = up;
+      l_tot[0] = l_tot[0] * f0 + at[(16 * NC + 1) * 64] * f1;
+#pragma unroll
+      for (int t = 0; t < NC; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[0][t][r] = o[0][t][r] * f0 + at[(16 * t + r) * 64] * f1;
+    }
+  }
+  if (p.splits > 1) {
+    if ((!FEW || my_block == 0) && row < p.rows) {
+      float* const rec = p.partial + diff_record(p, bh, row, split);
+#pragma unroll
+      for (int m = 0; m < MAPS; ++m) {
+#pragma unroll
+        for (int t = 0; t < NC; ++t)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const int col = 32 * t + 8 * q4 + 4 * half;
+            if (col < w) *(f32x4*)(rec + (map0 + m) * w + col) = f32x4{o[m][t][4 * q4], o[m][t][4 * q4 + 1], o[m][t][4 * q4 + 2], o[m][t][4 * q4 + 3]};
+          }
+        if (low) { rec[2 * w + 2 * (map0 + m)] = m_ref[m]; rec[2 * w + 2 * (map0 + m) + 1] = l_tot[m]; }
+      }
+    }
+    return;
+  }
+  const int head = hk * p.group + hg;
+  const float lam = p.lambda[head];
+  f32x16 res[NC];
+  if constexpr (FEW) {
+    // the second map's wavefront hands lambda o2 / l2 to the first's
+    __syncthreads();
+    if (wave == 1) {
+      const float f2 = lam * inverse_or_zero(l_tot[0]);
+#pragma unroll
+      for (int t = 0; t < NC; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) hand[(16 * t + r) * 64 + lane] = o[0][t][r] * f2;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const float f1 = inverse_or_zero(l_tot[0]);
+#pragma unroll
+    for (int t = 0; t < NC; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) res[t][r] = o[0][t][r] * f1 - hand[(16 * t + r) * 64 + lane];
+  } else {
+    const float f1 = inverse_or_zero(l_tot[0]), f2 = lam * inverse_or_zero(l_tot[MAPS - 1]);
+#pragma unroll
+    for (int t = 0; t < NC; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) res[t][r] = o[0][t][r] * f1 - o[MAPS - 1][t][r] * f2;
+  }
+  float sq = 0.f;
+#pragma unroll
+  for (int t = 0; t < NC; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sq = fmaf(res[t][r], res[t][r], sq);     // columns behind 2 d are zero
+  sq += other_half(sq, low);
+  const float r0 = p.gain ? p.out_scale * rsqrtf(sq / (float)w + p.eps) : p.out_scale;
+  if (row >= p.rows) return;
+  bf16* const out = (bf16*)p.out + ((size_t)b * p.l + i) * p.ldo + (size_t)head * w;
+#pragma unroll
+  for (int t = 0; t < NC; ++t)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const int col = 32 * t + 8 * q4 + 4 * half;
+      if (col >= w) continue;
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (bf16)(res[t][4 * q4 + e] * r0 * (p.gain ? p.gain[col + e] : 1.f));
+      *(bf16x4*)(out + col) = v;
+    }
+}
+
 // Joins the shares of the keys, in their order: a wavefront a row, lane j has columns j, j + 64, ...
 template <typename T>
 __global__ __launch_bounds__(256) void k_diff_join(DiffParams p, unsigned total) {
@@ -245,10 +521,17 @@ __global__ __launch_bounds__(256) void k_diff_join(DiffParams p, unsigned total)
   }
 }
 
-// Where the tiles leave the chip idle the keys are shared out over workgroups, at least 256 keys each
-static int diff_splits(long long tiles, int lk) {
-  const long long want = (512 + tiles - 1) / tiles, most = (lk + 255) / 256;
-  return (int)std::max(1LL, std::min(std::min(want, most), 64LL));
+// How a call is cut up: rows a workgroup takes, and over how many workgroups the keys of a row are shared out where the rows leave the chip idle (at
+// least 256 keys each)
+struct DiffPlan { bool few; int rows_a_tile, tiles, splits; };
+static DiffPlan diff_plan(int dtype, long long bh, int rows, int lk) {
+  DiffPlan a{};
+  a.few = dtype == AD_BF16 && bh * ((rows + 127) / 128) <= 256;
+  a.rows_a_tile = dtype == AD_F32 ? 16 : a.few ? 32 : 128;
+  a.tiles = (rows + a.rows_a_tile - 1) / a.rows_a_tile;
+  const long long tiles = bh * a.tiles, want = (512 + tiles - 1) / tiles, most = (lk + 255) / 256;
+  a.splits = (int)std::max(1LL, std::min(std::min(want, most), 64LL));
+  return a;
 }
 static bool diff_shape_ok(int batch, int l, int lk, int heads, int kv_heads, int d) {
   return batch >= 1 && l >= 1 && lk >= 1 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 1 && d <= 128 &&
@@ -258,35 +541,59 @@ static size_t diff_partial_bytes(long long bh, long long rows, int splits, int d
   return splits > 1 ? (size_t)(bh * rows * splits) * (4 * (size_t)d + 4) * sizeof(float) : 0;
 }
 
-template <typename T>
-static ad_status run_diff(DiffParams p, int batch, int splits, hipStream_t s) {
-  p.tiles = (p.rows + 15) / 16;
-  p.splits = splits;
-  p.split_keys = ((p.lk + splits - 1) / splits + 15) / 16 * 16;
-  p.div_tiles = make_fastdiv((unsigned)p.tiles);
-  p.div_splits = make_fastdiv((unsigned)splits);
-  const dim3 grid((unsigned)(batch * p.kv_heads) * (unsigned)p.tiles * (unsigned)splits);
-#define AD_DIFF(DT_)                                                                                                                   \
-  do {                                                                                                                                 \
-    constexpr int lds_bytes = 8 * 16 * (64 * ((2 * DT_ + 3) / 4) + 4) * 4;                                                             \
-    static std::atomic<bool> attr_set{false};                                                                                          \
-    if (lds_bytes > 65536 && !attr_set) {                                                                                              \
-      AD_HIP(hipFuncSetAttribute((const void*)k_diff_generic<T, DT_>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes));         \
-      attr_set = true;                                                                                                                 \
-    }                                                                                                                                  \
-    hipLaunchKernelGGL((k_diff_generic<T, DT_>), grid, dim3(512), lds_bytes, s, p);                                                    \
-  } while (0)
-  if (p.d <= 16) AD_DIFF(1);
-  else if (p.d <= 32) AD_DIFF(2);
-  else if (p.d <= 64) AD_DIFF(4);
-  else AD_DIFF(8);
-#undef AD_DIFF
-  AD_HIP(hipGetLastError());
-  if (splits > 1) {
-    const unsigned total = (unsigned)(batch * p.kv_heads) * (unsigned)p.rows;
-    hipLaunchKernelGGL((k_diff_join<T>), dim3((total + 3) / 4), dim3(256), 0, s, p, total);
-    AD_HIP(hipGetLastError());
+template <typename K>
+static ad_status launch_diff(K kern, int threads, int lds_bytes, std::atomic<bool>& attr_set, unsigned blocks, const DiffParams& p, hipStream_t s) {
+  if (lds_bytes > 65536 && !attr_set) {
+    AD_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes));
+    attr_set = true;
   }
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(threads), lds_bytes, s, p);
+  AD_HIP(hipGetLastError());
+  return AD_OK;
+}
+
+template <int DT>
+static ad_status run_diff_generic(const DiffParams& p, unsigned blocks, hipStream_t s) {
+  static std::atomic<bool> attr_set{false};
+  return launch_diff(k_diff_generic<float, DT>, 512, 8 * 16 * (64 * ((2 * DT + 3) / 4) + 4) * 4, attr_set, blocks, p, s);
+}
+
+template <int NC>
+static ad_status run_diff_mfma(const DiffParams& p, bool few, unsigned blocks, hipStream_t s) {
+  constexpr int lds_bytes = 2 * 2 * 64 * diff_pitch(NC);
+  static_assert(2 * (16 * NC + 2) * 64 * 4 <= lds_bytes, "the sums of two wavefronts");
+  static std::atomic<bool> set_few{false}, set_many{false};
+  return few ? launch_diff(k_diff_mfma<NC, true>, 256, lds_bytes, set_few, blocks, p, s) : launch_diff(k_diff_mfma<NC, false>, 256, lds_bytes, set_many, blocks, p, s);
+}
+
+static ad_status run_diff(int dtype, DiffParams p, const DiffPlan& plan, int batch, hipStream_t s) {
+  p.tiles = plan.tiles;
+  p.splits = plan.splits;
+  const int step = dtype == AD_BF16 ? 64 : 16;
+  p.split_keys = ((p.lk + p.splits - 1) / p.splits + step - 1) / step * step;
+  p.div_tiles = make_fastdiv((unsigned)p.tiles);
+  p.div_splits = make_fastdiv((unsigned)p.splits);
+  const unsigned blocks = (unsigned)(batch * p.kv_heads) * (unsigned)p.tiles * (unsigned)p.splits;
+  const int chunks = (p.d + 15) / 16;
+  ad_status st;
+  if (dtype == AD_BF16) {
+    if (chunks <= 2) st = run_diff_mfma<2>(p, plan.few, blocks, s);
+    else if (chunks == 3) st = run_diff_mfma<3>(p, plan.few, blocks, s);
+    else if (chunks == 4) st = run_diff_mfma<4>(p, plan.few, blocks, s);
+    else if (chunks == 5) st = run_diff_mfma<5>(p, plan.few, blocks, s);
+    else if (chunks == 6) st = run_diff_mfma<6>(p, plan.few, blocks, s);
+    else st = run_diff_mfma<8>(p, plan.few, blocks, s);
+  } else {
+    if (chunks <= 1) st = run_diff_generic<1>(p, blocks, s);
+    else if (chunks == 2) st = run_diff_generic<2>(p, blocks, s);
+    else if (chunks <= 4) st = run_diff_generic<4>(p, blocks, s);
+    else st = run_diff_generic<8>(p, blocks, s);
+  }
+  if (st != AD_OK || p.splits <= 1) return st;
+  const unsigned total = (unsigned)(batch * p.kv_heads) * (unsigned)p.rows;
+  if (dtype == AD_BF16) hipLaunchKernelGGL((k_diff_join<bf16>), dim3((total + 3) / 4), dim3(256), 0, s, p, total);
+  else hipLaunchKernelGGL((k_diff_join<float>), dim3((total + 3) / 4), dim3(256), 0, s, p, total);
+  AD_HIP(hipGetLastError());
   return AD_OK;
 }
 
@@ -299,7 +606,7 @@ extern "C" {
 size_t ad_diff_attention_workspace_bytes(int dtype, int batch, int l, int lk, int heads, int kv_heads, int head_dim) {
   if ((dtype != AD_BF16 && dtype != AD_F32) || !diff_shape_ok(batch, l, lk, heads, kv_heads, head_dim)) return 0;
   const long long rows = (long long)l * (heads / kv_heads), bh = (long long)batch * kv_heads;
-  return diff_partial_bytes(bh, rows, diff_splits(bh * ((rows + 15) / 16), lk), head_dim);
+  return diff_partial_bytes(bh, rows, diff_plan(dtype, bh, (int)rows, lk).splits, head_dim);
 }
 
 ad_status ad_diff_attention_forward(int dtype, const void* q, const void* k, const void* v, int batch, int l, int lk, int heads, int kv_heads,
@@ -313,6 +620,8 @@ ad_status ad_diff_attention_forward(int dtype, const void* q, const void* k, con
   if (head_dim % vn) AD_FAIL(AD_ERR_INVALID, "differential attention: head_dim must be a multiple of %d", vn);
   const long long w = 2LL * head_dim;
   if (ldq < heads * w || ldk < kv_heads * w || ldv < kv_heads * w || ldo < heads * w) AD_FAIL(AD_ERR_INVALID, "differential attention: bad leading dimension");
+  // the tile loads address 64 keys through 32-bit byte offsets from the first of them
+  if (dtype == AD_BF16 && (ldk >= (1 << 24) || ldv >= (1 << 24))) AD_FAIL(AD_ERR_INVALID, "differential attention: rows of keys or values too far apart");
   if ((ldq | ldk | ldv | ldo) % vn || (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15))
     AD_FAIL(AD_ERR_INVALID, "differential attention: tensors and rows must be aligned to 16 bytes");
   if (((uintptr_t)key_lens | (uintptr_t)lambda | (uintptr_t)norm_gain) % 4 || (uintptr_t)workspace % 16) AD_FAIL(AD_ERR_INVALID, "differential attention: misaligned argument");
@@ -329,11 +638,11 @@ ad_status ad_diff_attention_forward(int dtype, const void* q, const void* k, con
   p.div_group = make_fastdiv((unsigned)p.group);
   p.div_kv = make_fastdiv((unsigned)kv_heads);
   const long long bh = (long long)batch * kv_heads;
-  int splits = diff_splits(bh * ((p.rows + 15) / 16), lk);
-  if (splits > 1 && (!workspace || workspace_bytes < diff_partial_bytes(bh, p.rows, splits, head_dim))) splits = 1;
+  DiffPlan plan = diff_plan(dtype, bh, p.rows, lk);
+  if (plan.splits > 1 && (!workspace || workspace_bytes < diff_partial_bytes(bh, p.rows, plan.splits, head_dim))) plan.splits = 1;
   ProfLaunch pl(dtype == AD_BF16 ? "diff_attn_bf16" : "diff_attn_f32", 12.0 * batch * heads * head_dim * l * lk,
                 2.0 * esize(dtype) * batch * head_dim * (2.0 * l * heads + 2.0 * lk * kv_heads), (hipStream_t)stream, batch * l, lk, (int)(heads * w));
-  return dtype == AD_BF16 ? run_diff<bf16>(p, batch, splits, (hipStream_t)stream) : run_diff<float>(p, batch, splits, (hipStream_t)stream);
+  return run_diff(dtype, p, plan, batch, (hipStream_t)stream);
 }
 
 ad_status ad_diff_lambda(const float* q1, const float* k1, const float* q2, const float* k2, int n, float init, float* lambda) {

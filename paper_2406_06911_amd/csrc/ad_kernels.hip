@@ -582,21 +582,9 @@ __global__ __launch_bounds__(256) void k_igemm(IgemmParams p) {
 // wavefront's load covers 8 rows x 128 bytes = 1 KiB, written at m0 + lane * 16.  The loads are
 // issued from inline assembly so that the k-loop can wait for exactly the tile it is about to use.
 // =================================================================================================
-__device__ __forceinline__ void dma_load16(u32x4 rsrc, unsigned voffset, unsigned soffset, unsigned lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               :: "s"(lds_addr), "v"(voffset), "s"(rsrc), "s"(soffset) : "memory");
-}
 // A load whose data nobody wants: 64 pieces of 128 bytes are on their way from memory to the caches, 4 bytes of each to LDS
 __device__ __forceinline__ void dma_touch(u32x4 rsrc, unsigned voffset, unsigned lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds_addr), "v"(voffset), "s"(rsrc) : "memory");
-}
-__device__ __forceinline__ u32x4 make_rsrc_words(const void* base, unsigned bytes) {
-  const unsigned long long a = (unsigned long long)base;
-  return u32x4{(unsigned)a, (unsigned)(a >> 32) & 0xffffu, bytes, 0x00020000u};
-}
-// waits until at most n of this wavefront's vector-memory operations are outstanding (n < 64)
-template <int N> __device__ __forceinline__ void wait_vmcnt() {
-  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
 // Swizzle of the dense 128-byte LDS rows the load unit fills: row r keeps its 16-byte chunk c at position
@@ -2458,12 +2446,6 @@ void set_order_override(int order) { g_order_override = order; }
 // wavefront owns 32 queries.  Per 64-key tile: S^T = K Q^T (keys in accumulator registers, the
 // query in the lane), online softmax with one cross-half exchange, O^T += V^T P^T.
 // =================================================================================================
-__device__ __forceinline__ float other_half(float x, bool low) {
-  const unsigned u = __float_as_uint(x);
-  auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return __uint_as_float(low ? r[1] : r[0]);
-}
-
 constexpr int kAttnStage = 2 * 64 * kPitch;   // one K tile and one V^T tile (64 rows of 128 bytes + pad each)
 
 // four wavefronts per SIMD: with 32-bit running offsets instead of pointers the score and output tiles, the query
