@@ -13,6 +13,7 @@
 namespace ad {
 
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kDiffMaxSplits = 64;   // shares of the keys: a lane each when they are joined
 
 struct DiffParams {
   const void *q, *k, *v; void* out;
@@ -476,49 +477,64 @@ __global__ __launch_bounds__(256, NC <= 2 ? 3 : NC <= 4 ? 2 : 1) void k_diff_mfm
     }
 }
 
-// Joins the shares of the keys, in their order: a wavefront a row, lane j has columns j, j + 64, ...
+// Joins the shares of the keys, in their order.  A workgroup a row: the shares' references and sums give one factor each, then a thread has four
+// columns of a map (d threads) and every 256 / d-th share, and the shares' groups meet in LDS.
 template <typename T>
-__global__ __launch_bounds__(256) void k_diff_join(DiffParams p, unsigned total) {
-  const unsigned at = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (at >= total) return;
-  const unsigned bh = at / p.rows, row = at - bh * p.rows;
+__global__ __launch_bounds__(256) void k_diff_join(DiffParams p) {
+  __shared__ float factor[2][kDiffMaxSplits];
+  __shared__ f32x4 meet[256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const unsigned bh = blockIdx.x / (unsigned)p.rows, row = blockIdx.x - bh * p.rows;
   const unsigned b = fast_div(bh, p.div_kv), hk = bh - b * p.kv_heads;
-  const int w = 2 * p.d;
-  constexpr int CN = 4;
-  float acc[2][CN], den[2];
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    float most = -INFINITY;
-    for (int x = 0; x < p.splits; ++x) most = fmaxf(most, p.partial[diff_record(p, bh, row, x) + 2 * w + 2 * m]);
-    den[m] = 0.f;
-#pragma unroll
-    for (int c = 0; c < CN; ++c) acc[m][c] = 0.f;
-    for (int x = 0; x < p.splits; ++x) {
-      const float* const rec = p.partial + diff_record(p, bh, row, x);
-      const float f = most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rec[2 * w + 2 * m] - most);
-      den[m] += f * rec[2 * w + 2 * m + 1];
-#pragma unroll
-      for (int c = 0; c < CN; ++c)
-        if (lane + 64 * c < w) acc[m][c] += f * rec[m * w + lane + 64 * c];
-    }
-  }
+  const int d = p.d, w = 2 * d, n = p.splits;
   const unsigned query = fast_div(row, p.div_group), head = hk * p.group + row - query * p.group;
-  const float f1 = inverse_or_zero(den[0]), f2 = p.lambda[head] * inverse_or_zero(den[1]);
-  float sq = 0.f;
+  const float* const recs = p.partial + diff_record(p, bh, row, 0);
+  const size_t pitch = 4 * d + 4;
+  // quad `quad` of a record's 4 d sums, shares first, first + groups, ...; what is read first does not need the factors
+  const int groups = 256 / d, quad = tid % d, first = tid / d;
+  const bool on = first < groups;
+  constexpr int UN = 4;
+  f32x4 x[UN];
+  auto fetch = [&](int s0) {
 #pragma unroll
-  for (int c = 0; c < CN; ++c) {
-    acc[0][c] = acc[0][c] * f1 - acc[1][c] * f2;
-    sq = fmaf(acc[0][c], acc[0][c], sq);
+    for (int u = 0; u < UN; ++u)
+      if (on && s0 + u * groups < n) x[u] = *(const f32x4*)(recs + (size_t)(s0 + u * groups) * pitch + 4 * quad);
+  };
+  fetch(first);
+  if (wave < 2) {                                              // a wavefront a map; lane s: share s
+    const bool mine = lane < n;
+    const float m = mine ? recs[lane * pitch + 2 * w + 2 * wave] : -INFINITY, l = mine ? recs[lane * pitch + 2 * w + 2 * wave + 1] : 0.f;
+    float most = m;
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s, 64));
+    const float f = most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - most);
+    float inv = inverse_or_zero(wave_sum(f * l));
+    if (wave == 1) inv *= -p.lambda[head];
+    if (mine) factor[wave][lane] = f * inv;
   }
-  sq = wave_sum(sq);
+  __syncthreads();
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  const float* const f = factor[quad >= d / 2];
+  for (int s0 = first; on && s0 < n; s0 += UN * groups) {
+    if (s0 > first) fetch(s0);
+#pragma unroll
+    for (int u = 0; u < UN; ++u)
+      if (s0 + u * groups < n) acc += f[s0 + u * groups] * x[u];
+  }
+  meet[tid] = acc;
+  __syncthreads();
+  if (wave > 0) return;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const bool mine = lane < d / 2;                              // columns 4 lane .. 4 lane + 3 of the head
+  if (mine)
+    for (int g = 0; g < groups; ++g) o += meet[g * d + lane] + meet[g * d + d / 2 + lane];
+  const float sq = wave_sum(o[0] * o[0] + o[1] * o[1] + o[2] * o[2] + o[3] * o[3]);
   const float r = p.gain ? p.out_scale * rsqrtf(sq / (float)w + p.eps) : p.out_scale;
-  T* const out = (T*)p.out + ((size_t)b * p.l + query) * p.ldo + (size_t)head * w;
+  if (!mine) return;
+  typename Quad<T>::type res;
 #pragma unroll
-  for (int c = 0; c < CN; ++c) {
-    const int col = lane + 64 * c;
-    if (col < w) out[col] = from_f<T>(acc[0][c] * r * (p.gain ? p.gain[col] : 1.f));
-  }
+  for (int e = 0; e < 4; ++e) res[e] = from_f<T>(o[e] * r * (p.gain ? p.gain[4 * lane + e] : 1.f));
+  *(typename Quad<T>::type*)((T*)p.out + ((size_t)b * p.l + query) * p.ldo + (size_t)head * w + 4 * lane) = res;
 }
 
 // How a call is cut up: rows a workgroup takes, and over how many workgroups the keys of a row are shared out where the rows leave the chip idle (at
@@ -530,7 +546,7 @@ static DiffPlan diff_plan(int dtype, long long bh, int rows, int lk) {
   a.rows_a_tile = dtype == AD_F32 ? 16 : a.few ? 32 : 128;
   a.tiles = (rows + a.rows_a_tile - 1) / a.rows_a_tile;
   const long long tiles = bh * a.tiles, want = (512 + tiles - 1) / tiles, most = (lk + 255) / 256;
-  a.splits = (int)std::max(1LL, std::min(std::min(want, most), 64LL));
+  a.splits = (int)std::max(1LL, std::min(std::min(want, most), (long long)kDiffMaxSplits));
   return a;
 }
 static bool diff_shape_ok(int batch, int l, int lk, int heads, int kv_heads, int d) {
@@ -591,8 +607,8 @@ static ad_status run_diff(int dtype, DiffParams p, const DiffPlan& plan, int bat
   }
   if (st != AD_OK || p.splits <= 1) return st;
   const unsigned total = (unsigned)(batch * p.kv_heads) * (unsigned)p.rows;
-  if (dtype == AD_BF16) hipLaunchKernelGGL((k_diff_join<bf16>), dim3((total + 3) / 4), dim3(256), 0, s, p, total);
-  else hipLaunchKernelGGL((k_diff_join<float>), dim3((total + 3) / 4), dim3(256), 0, s, p, total);
+  if (dtype == AD_BF16) hipLaunchKernelGGL((k_diff_join<bf16>), dim3(total), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((k_diff_join<float>), dim3(total), dim3(256), 0, s, p);
   AD_HIP(hipGetLastError());
   return AD_OK;
 }
