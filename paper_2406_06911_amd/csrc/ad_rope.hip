@@ -21,26 +21,25 @@ constexpr int kRopeMaxDim = 128;   // widest head: the limit of the attention ke
 // v_sin_f32 / v_cos_f32 take turns; over one turn they are off by at most 1.3e-7 (rms 3.5e-8, measured at 2^20 phases), less than
 // an fp32 angle's own rounding, so fp32 tensors use them as well.
 //
-// A head is shared out over a power of two of lanes, each with two accesses of VN elements (up to 16 bytes each): the two sides of VN pairs
-// where the pairs lie half the rotated part apart, VN pairs in a row where they are neighbours; the part that is not rotated lies behind.
-// The norm's sums go over those lanes.  Such a group of lanes walks `slots`-th heads of its row and forms its angles once for all of them.
-// Bound by memory: every element is read once and written once; a lane may write where it has read, so q_out may be q.
+// A workgroup takes a few rows with all heads of q and k.  It asks for its elements, forms the sines and cosines of its rows once, in LDS, and the heads
+// read them from there.  A head is shared out over a power of two of lanes, each with two accesses of VN elements (up to 16 bytes each): the two sides of VN
+// pairs where the pairs lie half the rotated part apart, VN pairs in a row where they are neighbours; the part that is not rotated lies behind.  The norm's
+// sums go over those lanes.  Bound by memory: every element is read once and written once; a lane writes where it has read, so q_out may be q.
 // =================================================================================================
 struct RopeSide {
   const void* src; void* dst;
   const float *gain, *offset;
   int heads, ld, ldo;
-  int log_slots;                 // 2^log_slots groups of lanes share a row
-  unsigned blocks;
 };
 struct RopeParams {
-  RopeSide side[2];              // q, k
+  RopeSide q, k;
   const unsigned long long* table;
   const int* positions;
   long long sample_positions;    // positions of a sample, 0: shared
   unsigned rows, l;
-  FastDiv div_l;
-  int d, pairs, n_axes, axis_end[AD_ROPE_MAX_AXES];   // last pair of an axis + 1
+  FastDiv div_l, div_heads, div_pairs;
+  int d, pairs, axis_end[AD_ROPE_MAX_AXES];   // last pair of an axis + 1
+  int heads, block_rows;         // of q and k together; rows of a workgroup
   int units, log_lanes;          // lanes' shares of a head, lanes of a head
   float eps, amplitude, inv_d;
 };
@@ -63,15 +62,12 @@ __device__ __forceinline__ float head_sum(float v, int log_lanes) {
 template <typename T, int VN, int LAYOUT, int NORM>
 __global__ __launch_bounds__(256) void k_rope(RopeParams p) {
   typedef Access<T, VN> V;
-  const bool is_k = blockIdx.x >= p.side[0].blocks;
-  const RopeSide& s = p.side[is_k];
-  const unsigned block = blockIdx.x - (is_k ? p.side[0].blocks : 0u);
-  const int unit = threadIdx.x & ((1 << p.log_lanes) - 1);
-  const unsigned group = threadIdx.x >> p.log_lanes;
-  const int log_groups = 8 - p.log_lanes;
-  const unsigned row = (block << (log_groups - s.log_slots)) + (group >> s.log_slots);
-  const int slot = group & ((1 << s.log_slots) - 1);
-  const bool live = row < p.rows && unit < p.units;
+  typedef Access<float, VN> F;
+  extern __shared__ __attribute__((aligned(16))) float lds[];    // cosines [row][pair], sines [row][pair], then gain (and offset) of q and of k
+  const int tid = threadIdx.x;
+  const int unit = tid & ((1 << p.log_lanes) - 1), group = tid >> p.log_lanes, groups = 256 >> p.log_lanes;
+  const unsigned row0 = blockIdx.x * (unsigned)p.block_rows;
+  const int rows = min((unsigned)p.block_rows, p.rows - row0), items = rows * p.heads;
 
   // where this lane's two accesses lie in a head
   const int turning = p.pairs / VN;              // lanes with rotated pairs
@@ -84,65 +80,65 @@ __global__ __launch_bounds__(256) void k_rope(RopeParams p) {
     at_a = 2 * p.pairs + 2 * (unit - turning) * VN;
     at_b = at_a + VN;
   }
-  const bool has_a = live && at_a < p.d, has_b = live && at_b < p.d;
+  const bool has_a = at_a < p.d, has_b = at_b < p.d;
 
-  const T* const src = (const T*)s.src + (size_t)(live ? row : 0) * s.ld;
-  T* const dst = (T*)s.dst + (size_t)(live ? row : 0) * s.ldo;
   constexpr int UN = 4;                          // heads in flight
   V a[UN], b[UN];
-  const int step = 1 << s.log_slots;
-  auto fetch = [&](int h0) {
+  auto split = [&](int item, int& r, int& h) {
+    r = (int)fast_div((unsigned)item, p.div_heads);
+    h = item - r * p.heads;
+  };
+  auto fetch = [&](int first) {
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
-      const int h = h0 + u * step;
-      const bool on = h < s.heads;
-      if (on && has_a) a[u] = *(const V*)(src + (size_t)h * p.d + at_a);
-      if (on && has_b) b[u] = *(const V*)(src + (size_t)h * p.d + at_b);
+      const int item = first + u * groups;
+#pragma unroll
+      for (int e = 0; e < VN; ++e) { a[u].v[e] = from_f<T>(0.f); b[u].v[e] = from_f<T>(0.f); }
+      if (item >= items) continue;
+      int r, h;
+      split(item, r, h);
+      const bool is_k = h >= p.q.heads;
+      const T* const src = (const T*)(is_k ? p.k.src : p.q.src) + (size_t)(row0 + r) * (is_k ? p.k.ld : p.q.ld) + (size_t)(is_k ? h - p.q.heads : h) * p.d;
+      if (has_a) a[u] = *(const V*)(src + at_a);
+      if (has_b) b[u] = *(const V*)(src + at_b);
     }
   };
-#pragma unroll
-  for (int u = 0; u < UN; ++u)
-#pragma unroll
-    for (int e = 0; e < VN; ++e) { a[u].v[e] = from_f<T>(0.f); b[u].v[e] = from_f<T>(0.f); }
-  fetch(slot);
+  fetch(group);
 
-  float co[VN], si[VN];
-#pragma unroll
-  for (int e = 0; e < VN; ++e) { co[e] = 1.f; si[e] = 0.f; }
-  if (live && turns) {
-    const unsigned sample = fast_div(row, p.div_l);
-    const int* const pos = p.positions + (size_t)sample * p.sample_positions + (row - sample * p.l);
-    int n[AD_ROPE_MAX_AXES];
-#pragma unroll
-    for (int x = 0; x < AD_ROPE_MAX_AXES; ++x) n[x] = x < p.n_axes ? pos[(size_t)x * p.l] : 0;
-#pragma unroll
-    for (int e = 0; e < VN; ++e) {
-      const int pair = unit * VN + e;
-      const unsigned long long f = p.table[pair];
-      const int at = pair < p.axis_end[0] ? n[0] : (pair < p.axis_end[1] ? n[1] : n[2]);
-      const unsigned phase = (unsigned)(((unsigned long long)(long long)at * f) >> 32);
-      const float turn = (float)(int)phase * 0x1p-32f;
-      co[e] = __builtin_amdgcn_cosf(turn) * p.amplitude;
-      si[e] = __builtin_amdgcn_sinf(turn) * p.amplitude;
-    }
+  float* const cosines = lds;
+  float* const sines = lds + p.block_rows * p.pairs;
+  float* const gains = sines + p.block_rows * p.pairs;
+  for (int at = tid; at < rows * p.pairs; at += 256) {
+    const int r = (int)fast_div((unsigned)at, p.div_pairs), pair = at - r * p.pairs;
+    const unsigned row = row0 + r, sample = fast_div(row, p.div_l);
+    const int axis = (pair >= p.axis_end[0]) + (pair >= p.axis_end[1]);
+    const int n = p.positions[(size_t)sample * p.sample_positions + (size_t)axis * p.l + (row - sample * p.l)];
+    const unsigned long long f = p.table[pair];
+    const unsigned f_lo = (unsigned)f, f_hi = (unsigned)(f >> 32);
+    const unsigned phase = (unsigned)n * f_hi + __umulhi((unsigned)n, f_lo) - (n < 0 ? f_lo : 0u);     // bits 32 .. 63 of n * f
+    const float turn = (float)(int)phase * 0x1p-32f;
+    cosines[at] = __builtin_amdgcn_cosf(turn) * p.amplitude;
+    sines[at] = __builtin_amdgcn_sinf(turn) * p.amplitude;
   }
-  float ga[VN], gb[VN], oa[VN], ob[VN];
   if constexpr (NORM != ROPE_NO_NORM) {
-#pragma unroll
-    for (int e = 0; e < VN; ++e) {
-      ga[e] = s.gain && has_a ? s.gain[at_a + e] : 1.f;
-      gb[e] = s.gain && has_b ? s.gain[at_b + e] : 1.f;
-      oa[e] = NORM == AD_NORM_LAYER && s.offset && has_a ? s.offset[at_a + e] : 0.f;
-      ob[e] = NORM == AD_NORM_LAYER && s.offset && has_b ? s.offset[at_b + e] : 0.f;
+    constexpr int KINDS = NORM == AD_NORM_LAYER ? 4 : 2;
+    for (int at = tid; at < KINDS * p.d; at += 256) {
+      const int kind = at / p.d, e = at - kind * p.d;            // gain of q, gain of k, offset of q, offset of k
+      const float* const from = kind == 0 ? p.q.gain : kind == 1 ? p.k.gain : kind == 2 ? p.q.offset : p.k.offset;
+      gains[at] = from ? from[e] : (kind < 2 ? 1.f : 0.f);
     }
   }
+  __syncthreads();
 
-  for (int h0 = slot; h0 < s.heads; h0 += UN * step) {
-    if (h0 > slot) fetch(h0);
+  for (int first = group; first < items; first += UN * groups) {
+    if (first > group) fetch(first);
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
-      const int h = h0 + u * step;
-      if (h >= s.heads) break;
+      const int item = first + u * groups;
+      if (item >= items) break;
+      int row, h;
+      split(item, row, h);
+      const bool is_k = h >= p.q.heads;
       float x[VN], y[VN];
 #pragma unroll
       for (int e = 0; e < VN; ++e) { x[e] = to_f(a[u].v[e]); y[e] = to_f(b[u].v[e]); }
@@ -162,40 +158,46 @@ __global__ __launch_bounds__(256) void k_rope(RopeParams p) {
 #pragma unroll
         for (int e = 0; e < VN; ++e) sq = fmaf(x[e], x[e], fmaf(y[e], y[e], sq));
         const float r = rsqrtf(head_sum(sq, p.log_lanes) * p.inv_d + p.eps);
+        const float* const gain = gains + (is_k ? p.d : 0);
+        F ga, gb, oa{}, ob{};
+        if (has_a) ga = *(const F*)(gain + at_a);
+        if (has_b) gb = *(const F*)(gain + at_b);
+        if constexpr (NORM == AD_NORM_LAYER) {
+          if (has_a) oa = *(const F*)(gain + 2 * p.d + at_a);
+          if (has_b) ob = *(const F*)(gain + 2 * p.d + at_b);
+        }
 #pragma unroll
         for (int e = 0; e < VN; ++e) {
-          x[e] = fmaf(x[e] * r, ga[e], oa[e]);
-          y[e] = fmaf(y[e] * r, gb[e], ob[e]);
+          x[e] = NORM == AD_NORM_LAYER ? fmaf(x[e] * r, ga.v[e], oa.v[e]) : x[e] * r * ga.v[e];
+          y[e] = NORM == AD_NORM_LAYER ? fmaf(y[e] * r, gb.v[e], ob.v[e]) : y[e] * r * gb.v[e];
         }
       }
       if (turns) {
-        if constexpr (LAYOUT == AD_ROPE_HALF) {
+        const F co = *(const F*)(cosines + row * p.pairs + unit * VN), si = *(const F*)(sines + row * p.pairs + unit * VN);
+        if constexpr (LAYOUT == AD_ROPE_HALF || VN == 1) {
 #pragma unroll
           for (int e = 0; e < VN; ++e) {
             const float xe = x[e], ye = y[e];
-            x[e] = fmaf(xe, co[e], -(ye * si[e]));
-            y[e] = fmaf(ye, co[e], xe * si[e]);
+            x[e] = fmaf(xe, co.v[e], -(ye * si.v[e]));
+            y[e] = fmaf(ye, co.v[e], xe * si.v[e]);
           }
-        } else if constexpr (VN == 1) {
-          const float xe = x[0], ye = y[0];
-          x[0] = fmaf(xe, co[0], -(ye * si[0]));
-          y[0] = fmaf(ye, co[0], xe * si[0]);
         } else {
 #pragma unroll
           for (int e = 0; e < VN; e += 2) {
             const float x0 = x[e], x1 = x[e + 1], y0 = y[e], y1 = y[e + 1];
-            x[e] = fmaf(x0, co[e / 2], -(x1 * si[e / 2]));
-            x[e + 1] = fmaf(x1, co[e / 2], x0 * si[e / 2]);
-            y[e] = fmaf(y0, co[(VN + e) / 2], -(y1 * si[(VN + e) / 2]));
-            y[e + 1] = fmaf(y1, co[(VN + e) / 2], y0 * si[(VN + e) / 2]);
+            x[e] = fmaf(x0, co.v[e / 2], -(x1 * si.v[e / 2]));
+            x[e + 1] = fmaf(x1, co.v[e / 2], x0 * si.v[e / 2]);
+            y[e] = fmaf(y0, co.v[(VN + e) / 2], -(y1 * si.v[(VN + e) / 2]));
+            y[e + 1] = fmaf(y1, co.v[(VN + e) / 2], y0 * si.v[(VN + e) / 2]);
           }
         }
       }
       V wa, wb;
 #pragma unroll
       for (int e = 0; e < VN; ++e) { wa.v[e] = from_f<T>(x[e]); wb.v[e] = from_f<T>(y[e]); }
-      if (has_a) *(V*)(dst + (size_t)h * p.d + at_a) = wa;
-      if (has_b) *(V*)(dst + (size_t)h * p.d + at_b) = wb;
+      T* const dst = (T*)(is_k ? p.k.dst : p.q.dst) + (size_t)(row0 + row) * (is_k ? p.k.ldo : p.q.ldo) + (size_t)(is_k ? h - p.q.heads : h) * p.d;
+      if (has_a) *(V*)(dst + at_a) = wa;
+      if (has_b) *(V*)(dst + at_b) = wb;
     }
   }
 }
@@ -239,7 +241,7 @@ static ad_status launch_rope(const char* name, int dtype, int norm, const ad_rop
   if (!q || !q_out || (kv_heads > 0 && (!k || !k_out))) AD_FAIL(AD_ERR_INVALID, "%s: null pointer", name);
   if (batch < 1 || l < 1 || heads < 1 || kv_heads < 0 || d < 1 || d > kRopeMaxDim || (long long)batch * l > 0x7fffffffLL)
     AD_FAIL(AD_ERR_INVALID, "%s: bad shape (head_dim 1..%d)", name, kRopeMaxDim);
-  if ((long long)heads * d > 0x7fffffffLL || (long long)kv_heads * d > 0x7fffffffLL) AD_FAIL(AD_ERR_INVALID, "%s: too many heads", name);
+  if (((long long)heads + kv_heads) * d > 0x7fff0000LL) AD_FAIL(AD_ERR_INVALID, "%s: too many heads", name);
   if (ldq < heads * d || ldq_out < heads * d || (kv_heads > 0 && (ldk < kv_heads * d || ldk_out < kv_heads * d))) AD_FAIL(AD_ERR_INVALID, "%s: bad leading dimension", name);
   if ((q == q_out && ldq != ldq_out) || (kv_heads > 0 && k == k_out && ldk != ldk_out)) AD_FAIL(AD_ERR_INVALID, "%s: in place, both leading dimensions are the same", name);
   if (kv_heads > 0 && q_out == k_out) AD_FAIL(AD_ERR_INVALID, "%s: q_out and k_out are the same", name);
@@ -258,7 +260,6 @@ static ad_status launch_rope(const char* name, int dtype, int norm, const ad_rop
       p.axis_end[a] = pairs;
     }
     if (2 * pairs > d) AD_FAIL(AD_ERR_INVALID, "%s: the axes turn %d elements of a head of %d", name, 2 * pairs, d);
-    p.n_axes = cfg->n_axes;
     p.amplitude = (float)rope_amplitude(*cfg);
   }
   if (norm != ROPE_NO_NORM) {
@@ -279,24 +280,24 @@ static ad_status launch_rope(const char* name, int dtype, int norm, const ad_rop
   p.d = d; p.pairs = pairs;
   p.table = (const unsigned long long*)table;
   p.positions = positions;
-  p.sample_positions = per_sample ? (long long)p.n_axes * l : 0;
+  p.sample_positions = cfg && per_sample ? (long long)cfg->n_axes * l : 0;
   p.eps = eps; p.inv_d = 1.f / (float)d;
-  p.side[0] = RopeSide{q, q_out, q_gain, q_offset, heads, ldq, ldq_out, 0, 0};
-  p.side[1] = RopeSide{k, k_out, k_gain, k_offset, kv_heads, ldk, ldk_out, 0, 0};
-  const int log_groups = 8 - p.log_lanes;
-  for (auto& side : p.side) {
-    if (side.heads == 0) continue;
-    // a group of lanes takes four heads of a row; where that leaves the chip idle, fewer
-    while ((4 << side.log_slots) < side.heads && side.log_slots < log_groups) ++side.log_slots;
-    while ((1 << side.log_slots) < side.heads && side.log_slots < log_groups && ((unsigned long long)p.rows << (side.log_slots + p.log_lanes)) < 256 * 1024) ++side.log_slots;
-    const int rows_a_block = 1 << (log_groups - side.log_slots);
-    side.blocks = (p.rows + rows_a_block - 1) / rows_a_block;
-  }
+  p.q = RopeSide{q, q_out, q_gain, q_offset, heads, ldq, ldq_out};
+  p.k = RopeSide{k, k_out, k_gain, k_offset, kv_heads, ldk, ldk_out};
+  p.heads = heads + kv_heads;
+  p.div_heads = make_fastdiv((unsigned)p.heads);
+  p.div_pairs = make_fastdiv((unsigned)std::max(pairs, 1));
+  // rows of a workgroup: what its lanes hold in flight at once, as far as the sines and cosines stay below 16 KiB; where that leaves CUs idle, fewer
+  const int in_flight = 4 * (256 >> p.log_lanes);
+  int block_rows = std::max(1, in_flight / p.heads);
+  if (pairs > 0) block_rows = std::min(block_rows, std::max(1, 2048 / pairs));
+  p.block_rows = (int)std::min<long long>(block_rows, std::max(1u, p.rows / 512));
+  const size_t lds_bytes = (size_t)(2 * p.block_rows * pairs + (norm == ROPE_NO_NORM ? 0 : 4 * d)) * 4;
   const double elements = (double)p.rows * (heads + kv_heads) * d;
   ProfLaunch pl(norm == ROPE_NO_NORM ? "rope" : "qk_norm_rope", 0, 2.0 * es * elements, s);
-  const dim3 grid(p.side[0].blocks + p.side[1].blocks);
+  const dim3 grid((p.rows + p.block_rows - 1) / p.block_rows);
   const int layout = cfg ? cfg->layout : AD_ROPE_HALF;
-#define AD_ROPE_RUN(T_, VN_, LAYOUT_, NORM_) hipLaunchKernelGGL((k_rope<T_, VN_, LAYOUT_, NORM_>), grid, dim3(256), 0, s, p)
+#define AD_ROPE_RUN(T_, VN_, LAYOUT_, NORM_) hipLaunchKernelGGL((k_rope<T_, VN_, LAYOUT_, NORM_>), grid, dim3(256), lds_bytes, s, p)
 #define AD_ROPE_NORM(T_, VN_, LAYOUT_)                                                \
   if (norm == ROPE_NO_NORM) AD_ROPE_RUN(T_, VN_, LAYOUT_, ROPE_NO_NORM);              \
   else if (norm == AD_NORM_RMS) AD_ROPE_RUN(T_, VN_, LAYOUT_, AD_NORM_RMS);           \
