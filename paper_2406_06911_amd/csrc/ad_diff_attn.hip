@@ -35,10 +35,6 @@ __device__ __forceinline__ size_t diff_record(const DiffParams& p, unsigned bh, 
 template <typename T> struct Quad;
 template <> struct Quad<float> { typedef f32x4 type; };
 template <> struct Quad<bf16> { typedef bf16x4 type; };
-template <typename T> __device__ __forceinline__ f32x4 load_quad(const T* at) {
-  const typename Quad<T>::type raw = *(const typename Quad<T>::type*)at;
-  return f32x4{to_f(raw[0]), to_f(raw[1]), to_f(raw[2]), to_f(raw[3])};
-}
 __device__ __forceinline__ float group_max(float v) {     // over the four lanes 16 apart that hold a row
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   return fmaxf(v, __shfl_xor(v, 32, 64));
@@ -48,13 +44,14 @@ __device__ __forceinline__ float group_max(float v) {     // over the four lanes
 __device__ __forceinline__ float inverse_or_zero(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // =================================================================================================
-// Any head width up to 128, on fp32 MFMA: 16 rows a workgroup, eight wavefronts share the keys out in blocks of 16.  Scores are computed
-// transposed (a lane owns a row), so the probabilities are the B operand of the product with v as they stand.  Column 4 m + e of a 64-wide
-// run of v is row m of the e-th of four accumulator tiles: a lane's 16-byte load feeds four tiles.
+// fp32: 16 rows a workgroup, four wavefronts share the keys out in blocks of 16.  Scores are computed transposed (a lane owns a row), so the
+// probabilities are the B operand of the product with v as they stand.  Column 4 m + e of a 64-wide run of v is row m of the e-th of four
+// accumulator tiles: a lane's 16-byte load feeds four tiles.  An fp32 MFMA takes 32 cycles for 2 KFLOP, so operands come straight from the
+// caches into registers, those of the next block while this one is multiplied.
 // =================================================================================================
-template <typename T, int DT>
-__global__ __launch_bounds__(512) void k_diff_generic(DiffParams p) {
-  constexpr int NW = 8, VT = (2 * DT + 3) / 4, PITCH = 64 * VT + 4;
+template <int DT>
+__global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p) {
+  constexpr int NW = 4, VT = (2 * DT + 3) / 4, PITCH = 64 * VT + 4;
   extern __shared__ __attribute__((aligned(16))) float part[];       // [wave][row][PITCH]: one map's sums; behind the columns m and l
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -73,15 +70,15 @@ __global__ __launch_bounds__(512) void k_diff_generic(DiffParams p) {
   const int last = min((int)tile * 16 + 15, p.rows - 1);
   const int from = split * p.split_keys, to = min(from + p.split_keys, limit_of((int)fast_div((unsigned)last, p.div_group)));
 
-  const T* const qrow = (const T*)p.q + ((size_t)b * p.l + i) * p.ldq + (size_t)(hk * p.group + hg) * w;
-  const T* const kbase = (const T*)p.k + (size_t)b * p.lk * p.ldk + (size_t)hk * w;
-  const T* const vbase = (const T*)p.v + (size_t)b * p.lk * p.ldv + (size_t)hk * w;
+  const float* const qrow = (const float*)p.q + ((size_t)b * p.l + i) * p.ldq + (size_t)(hk * p.group + hg) * w;
+  const float* const kbase = (const float*)p.k + (size_t)b * p.lk * p.ldk + (size_t)hk * w;
+  const float* const vbase = (const float*)p.v + (size_t)b * p.lk * p.ldv + (size_t)hk * w;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 qf[2][DT];
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int c = 0; c < DT; ++c) qf[m][c] = live && 16 * c + 4 * g < d ? load_quad(qrow + m * d + 16 * c + 4 * g) : zero;
+    for (int c = 0; c < DT; ++c) qf[m][c] = live && 16 * c + 4 * g < d ? *(const f32x4*)(qrow + m * d + 16 * c + 4 * g) : zero;
 
   f32x4 o[2][VT][4];
   float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
@@ -92,26 +89,43 @@ __global__ __launch_bounds__(512) void k_diff_generic(DiffParams p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[m][t][e] = zero;
 
-  for (int key0 = from + 16 * wave; key0 < to; key0 += 16 * NW) {
-    const T* const krow = kbase + (size_t)min(key0 + r16, len - 1) * p.ldk;
-    f32x4 s[2];
+  // what the end needs is asked for now
+  const int my_row = tid >> 4, c0 = 4 * (tid & 15);
+  const int out_row = tile * 16 + my_row, out_rowc = min(out_row, p.rows - 1);
+  const int query = fast_div((unsigned)out_rowc, p.div_group), head = hk * p.group + out_rowc - query * p.group;
+  const float lam = p.lambda[head];
+  f32x4 gain[VT];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      s[m] = zero;
+  for (int t = 0; t < VT; ++t)
 #pragma unroll
-      for (int c = 0; c < DT; ++c) {
-        const f32x4 kf = 16 * c + 4 * g < d ? load_quad(krow + m * d + 16 * c + 4 * g) : zero;
-        Mma16<float>::run(kf, qf[m][c], s[m]);
-      }
-    }
-    f32x4 vf[VT][4];                             // [run of 64 columns][key 4 g + r]
+    for (int e = 0; e < 4; ++e) gain[t][e] = p.gain && 64 * t + c0 < w ? p.gain[64 * t + c0 + e] : 1.f;
+
+  f32x4 kf[2][DT], vf[VT][4];                      // of a block: k [map][chunk of row r16], v [run of 64 columns][key 4 g + r]
+  auto fetch_k = [&](int key0) {
+    const float* const krow = kbase + (size_t)min(key0 + r16, len - 1) * p.ldk;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int c = 0; c < DT; ++c) kf[m][c] = 16 * c + 4 * g < d ? *(const f32x4*)(krow + m * d + 16 * c + 4 * g) : zero;
+  };
+  auto fetch_v = [&](int key0) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int key = key0 + 4 * g + r;
-      const T* const vrow = vbase + (size_t)min(key, len - 1) * p.ldv;
+      const float* const vrow = vbase + (size_t)min(key, len - 1) * p.ldv;
 #pragma unroll
-      for (int t = 0; t < VT; ++t) vf[t][r] = key < len && 64 * t + 4 * r16 < w ? load_quad(vrow + 64 * t + 4 * r16) : zero;
+      for (int t = 0; t < VT; ++t) vf[t][r] = key < len && 64 * t + 4 * r16 < w ? *(const f32x4*)(vrow + 64 * t + 4 * r16) : zero;
     }
+  };
+  if (from + 16 * wave < to) { fetch_k(from + 16 * wave); fetch_v(from + 16 * wave); }
+  for (int key0 = from + 16 * wave; key0 < to; key0 += 16 * NW) {
+    const int next = key0 + 16 * NW;
+    f32x4 s[2] = {zero, zero};
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) Mma16<float>::run(kf[m][c], qf[m][c], s[m]);
+    if (next < to) fetch_k(next);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       float most = -INFINITY;
@@ -127,21 +141,27 @@ __global__ __launch_bounds__(512) void k_diff_generic(DiffParams p) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) { s[m][r] = __builtin_amdgcn_exp2f(s[m][r] - ref); add += s[m][r]; }
       sum[m] = sum[m] * keep + add;              // of this lane's keys; the four groups are added at the end
+      if (__builtin_amdgcn_ballot_w64(keep != 1.f) != 0) {
+#pragma unroll
+        for (int t = 0; t < VT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[m][t][e] *= keep;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int t = 0; t < VT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          o[m][t][e] *= keep;
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[m][t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[t][r][e], s[m][r], o[m][t][e], 0, 0, 0);
-        }
-    }
+          for (int m = 0; m < 2; ++m) o[m][t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[t][r][e], s[m][r], o[m][t][e], 0, 0, 0);
+    if (next < to) fetch_v(next);
   }
 
-  // the wavefronts' sums meet in LDS, a map at a time; 32 threads take a row, columns c, c + 32, ...
-  const int my_row = tid >> 5, c0 = tid & 31;
-  constexpr int CN = 2 * VT;
-  float acc[2][CN], tops[2], sums[2];
+  // the wavefronts' sums meet in LDS, a map at a time; 16 threads take a row, columns 4 c .. 4 c + 3 of every run of 64
+  f32x4 acc[2][VT];
+  float tops[2], sums[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     sum[m] += __shfl_xor(sum[m], 16, 64);
@@ -158,7 +178,7 @@ __global__ __launch_bounds__(512) void k_diff_generic(DiffParams p) {
 #pragma unroll
     for (int x = 0; x < NW; ++x) most = fmaxf(most, part[(x * 16 + my_row) * PITCH + 64 * VT]);
 #pragma unroll
-    for (int c = 0; c < CN; ++c) acc[m][c] = 0.f;
+    for (int t = 0; t < VT; ++t) acc[m][t] = zero;
     float den = 0.f;
 #pragma unroll
     for (int x = 0; x < NW; ++x) {
@@ -166,300 +186,347 @@ __global__ __launch_bounds__(512) void k_diff_generic(DiffParams p) {
       const float f = most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(from_wave[64 * VT] - most);
       den += f * from_wave[64 * VT + 1];
 #pragma unroll
-      for (int c = 0; c < CN; ++c) acc[m][c] += f * from_wave[c0 + 32 * c];
+      for (int t = 0; t < VT; ++t) acc[m][t] += f * *(const f32x4*)(from_wave + 64 * t + c0);
     }
     tops[m] = most; sums[m] = den;
   }
-  const int out_row = tile * 16 + my_row;
   if (out_row >= p.rows) return;
   if (p.splits > 1) {
     float* const rec = p.partial + diff_record(p, bh, out_row, split);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
 #pragma unroll
-      for (int c = 0; c < CN; ++c)
-        if (c0 + 32 * c < w) rec[m * w + c0 + 32 * c] = acc[m][c];
+      for (int t = 0; t < VT; ++t)
+        if (64 * t + c0 < w) *(f32x4*)(rec + m * w + 64 * t + c0) = acc[m][t];
       if (c0 == 0) { rec[2 * w + 2 * m] = tops[m]; rec[2 * w + 2 * m + 1] = sums[m]; }
     }
     return;
   }
-  const int query = fast_div((unsigned)out_row, p.div_group), head = hk * p.group + out_row - query * p.group;
-  const float f1 = inverse_or_zero(sums[0]), f2 = p.lambda[head] * inverse_or_zero(sums[1]);
+  const float f1 = inverse_or_zero(sums[0]), f2 = lam * inverse_or_zero(sums[1]);
   float sq = 0.f;
 #pragma unroll
-  for (int c = 0; c < CN; ++c) {
-    acc[0][c] = c0 + 32 * c < w ? acc[0][c] * f1 - acc[1][c] * f2 : 0.f;
-    sq = fmaf(acc[0][c], acc[0][c], sq);
+  for (int t = 0; t < VT; ++t) {                               // columns behind 2 d are zero
+    acc[0][t] = acc[0][t] * f1 - acc[1][t] * f2;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sq = fmaf(acc[0][t][e], acc[0][t][e], sq);
   }
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) sq += __shfl_xor(sq, x, 64);
+  for (int x = 8; x > 0; x >>= 1) sq += __shfl_xor(sq, x, 64);
   const float r = p.gain ? p.out_scale * rsqrtf(sq / (float)w + p.eps) : p.out_scale;
-  T* const out = (T*)p.out + ((size_t)b * p.l + query) * p.ldo + (size_t)head * w;
+  float* const out = (float*)p.out + ((size_t)b * p.l + query) * p.ldo + (size_t)head * w;
 #pragma unroll
-  for (int c = 0; c < CN; ++c) {
-    const int col = c0 + 32 * c;
-    if (col < w) out[col] = from_f<T>(acc[0][c] * r * (p.gain ? p.gain[col] : 1.f));
+  for (int t = 0; t < VT; ++t) {
+    const int col = 64 * t + c0;
+    if (col >= w) continue;
+    *(f32x4*)(out + col) = acc[0][t] * r * gain[t];
   }
 }
 
 // =================================================================================================
-// bf16.  Tiles of 64 keys and their values are brought into LDS by the load unit, two stages.  A tile of k and one of v have the same shape: 64 rows of the
+// bf16.  Tiles of 64 keys and their values are brought into LDS by the load unit, two of each.  A tile of k and one of v have the same shape: 64 rows of the
 // head's 2 d columns (k1 | k2), on a pitch of 128, 256 or 512 bytes; columns behind 2 d and keys behind the sample's length read as zeros.  Scores are
 // computed transposed (S^T = K Q^T, a lane owns a row), so the probabilities are the B operand of O^T += V^T P^T as they stand; V^T fragments are read from
 // the row-major tile by the transposing LDS read, four keys of a column at a time.
+//
+// A wavefront owns 32 rows and one map, WR x 2 of them share the tiles; the second map's sums go to the first's wavefront through LDS at the end.  (Both maps
+// in a wavefront read every fragment of v for two products, but the sums of both, 2 x 2 d a row, leave no registers to overlap anything with: 2304 x 2304, 5 heads
+// of 2 x 64, two samples 66 us against 53.)  WB = 2, few rows: half of the wavefronts take every other tile half.
+//
+// A step of 32 keys is one straight line of MFMAs, the scores of the next block and the products of the block before, with the exponentials of this
+// block between them; the order is pinned, left alone the exponentials gather behind the MFMAs.  So k runs a tile ahead of v, and a barrier every two steps is enough.
 //
 // The exponential's reference need not be the running maximum: any value near it gives the same quotient.  It is the exact maximum of the first 32 keys
 // that a row sees, and is raised (and what has been summed rescaled) when a block's sum of weights reaches 2^24, so the steady state computes no
 // maximum.  A row sees a prefix of its keys, so where it sees any of a share, it sees the first.
 //
-// A wavefront owns 32 rows and both maps: a fragment of v serves two products.  FEW: for few rows, a workgroup takes 32 rows, and its four wavefronts take a
-// map and every other block of 32 keys each; their sums meet in LDS.
+// Probabilities are rounded to bf16 for the product with v, and the row's sum is of the rounded ones (half the instructions of a sum in front of the
+// rounding; the weights then add up to 1); scores, sums and references are fp32; q is not scaled in front of the product (a rounding less).
 //
-// Probabilities are rounded to bf16 for the product with v, scores, sums and references are fp32; q is not scaled in front of the product (a rounding less).
+// Bound: narrow heads by vector instructions (55 a step beside 6 MFMAs at d = 32), wide ones by the MFMAs, of which 12 d of the 12 d + exponentials operations
+// are counted; at 9216 x 9216 the clock falls to 1.9 GHz.  us: 2 x 9216 x 9216, 5 heads of 2 x 32 375 (870 TFLOP/s), 2 x 2304 x 2304, 5 of 2 x 64 53 (775; 180
+// workgroups on 256 CUs), 1511 x 6007 causal, 8 of 2 x 128 on 2 152 (640; 190 workgroups), one token x 8190 14.
 // =================================================================================================
+// f(0), f(1), .. f(N - 1) with constants: a loop of this length is not unrolled by itself, and arrays indexed in it would go to memory
+template <int N, typename F> __device__ __forceinline__ void unrolled(F&& f) {
+  if constexpr (N > 0) {
+    unrolled<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
 constexpr int diff_pitch(int nc) { return nc <= 2 ? 128 : nc <= 4 ? 256 : 512; }
-constexpr float kDiffBig = 16777216.f;
+constexpr float kDiffBig = 16777216.f;   // 2^24
 
-template <int NC, bool FEW>
-__global__ __launch_bounds__(256, NC <= 2 ? 3 : NC <= 4 ? 2 : 1) void k_diff_mfma(DiffParams p) {
-  constexpr int PITCH = diff_pitch(NC), CPR = PITCH / 16, TILE = 64 * PITCH, STAGE = 2 * TILE, LPT = TILE / 4096;
-  constexpr int MAPS = FEW ? 1 : 2, ROWS = FEW ? 32 : 128;
-  extern __shared__ __attribute__((aligned(128))) char lds[];
+template <int NC, int WR, int WB, int OCC>
+__global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) {
+  constexpr int PITCH = diff_pitch(NC), CPR = PITCH / 16, KEYS = 64 * WB, TILE = KEYS * PITCH, NW = 2 * WR * WB, LPT = TILE / 1024 / NW;
+  static_assert(LPT >= 1, "every wavefront loads");
+  extern __shared__ __attribute__((aligned(128))) char lds[];      // two tiles of k, two of v
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const bool low = half == 0;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int map0 = FEW ? wave & 1 : 0, my_block = wave >> 1;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), map = wave & 1, my_block = (wave >> 1) % WB, row_wave = (wave >> 1) / WB;
   const unsigned vid = xcd_remap(blockIdx.x, gridDim.x);
   const unsigned bt = fast_div(vid, p.div_splits), split = vid - bt * p.splits;
   const unsigned bh = fast_div(bt, p.div_tiles), tile = bt - bh * p.tiles;
   const unsigned b = fast_div(bh, p.div_kv), hk = bh - b * p.kv_heads;
-  const int d = p.d, w = 2 * d, d8 = d >> 3;
+  const int d = p.d, w = 2 * d;
   const int len = __builtin_amdgcn_readfirstlane(p.key_lens ? min(max(p.key_lens[b], 0), p.lk) : p.lk);
   auto limit_of = [&](int row) {
     return p.causal ? min(max((int)fast_div((unsigned)min(row, p.rows - 1), p.div_group) + len - p.l + 1, 0), len) : len;
   };
-  const int row0 = tile * ROWS + (FEW ? 0 : wave * 32), row = row0 + l32;
+  const int row0 = tile * (32 * WR) + 32 * row_wave, row = row0 + l32;
   const int rowc = min(row, p.rows - 1);                       // rows behind the last repeat it, and are not stored
   const int i = (int)fast_div((unsigned)rowc, p.div_group), hg = rowc - i * p.group;
-  const int limit = limit_of(row), lim_first = limit_of(row0), lim_last = limit_of(row0 + 31);
-  const int from = split * p.split_keys, to = min(from + p.split_keys, limit_of(tile * ROWS + ROWS - 1));
-  const int ntiles = to > from ? (to - from + 63) >> 6 : 0;
+  const int limit = limit_of(row), lim_first = limit_of(row0);
+  const int from = split * p.split_keys, to = min(from + p.split_keys, limit_of(tile * (32 * WR) + 32 * WR - 1));
+  const int ntiles = to > from ? (to - from + KEYS - 1) / KEYS : 0;
 
   // ---- tile loads
   const bf16* const kbase = (const bf16*)p.k + (size_t)b * p.lk * p.ldk + (size_t)hk * w;
   const bf16* const vbase = (const bf16*)p.v + (size_t)b * p.lk * p.ldv + (size_t)hk * w;
-  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
-  auto issue = [&](int t, int stage) {
-    const int key0 = from + 64 * t, n = min(64, len - key0);
-    const u32x4 rk = make_rsrc_words(kbase + (size_t)key0 * p.ldk, (unsigned)((n - 1) * p.ldk + w) * 2u);
-    const u32x4 rv = make_rsrc_words(vbase + (size_t)key0 * p.ldv, (unsigned)((n - 1) * p.ldv + w) * 2u);
-    const unsigned at = lds_base + stage * STAGE + wave * 1024u;
+  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds + wave * 1024u;
+  struct Stream { const bf16* at; int left; };                 // the next tile, and the keys from its first on
+  Stream next_k{kbase + (size_t)from * p.ldk, len - from}, next_v{vbase + (size_t)from * p.ldv, len - from};
+  auto issue = [&](Stream& n, int ld, unsigned at, auto swizzle) __attribute__((always_inline)) {
+    u32x4 rsrc = make_rsrc_words(n.at, (unsigned)((min(n.left, KEYS) - 1) * ld + w) * 2u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rsrc[e] = __builtin_amdgcn_readfirstlane(rsrc[e]);     // a descriptor lies in scalar registers
 #pragma unroll
     for (int x = 0; x < LPT; ++x) {
-      const int id = (x * 4 + wave) * 64 + lane, r = id / CPR, pos = id % CPR;
-      const int ck = pos ^ (PITCH == 128 ? (r >> 1) & 7 : r & 15), cv = pos ^ (PITCH == 128 ? (r << 1) & 4 : (r & 3) << 2);
-      dma_load16(rk, ck * 8 < w ? (unsigned)(r * p.ldk) * 2u + ck * 16u : kOob, 0u, at + x * 4096u);
-      dma_load16(rv, cv * 8 < w ? (unsigned)(r * p.ldv) * 2u + cv * 16u : kOob, 0u, at + TILE + x * 4096u);
+      const int id = (x * NW + wave) * 64 + lane, r = id / CPR, c = (id % CPR) ^ swizzle(r);
+      dma_load16(rsrc, c * 8 < w ? (unsigned)(r * ld) * 2u + c * 16u : kOob, 0u, at + x * NW * 1024u);
     }
+    n.at += (size_t)KEYS * ld;
+    n.left -= KEYS;
   };
-  if (ntiles > 0) issue(0, 0);
+  auto issue_k = [&](int slot) { issue(next_k, p.ldk, lds_base + slot * TILE, [](int r) { return PITCH == 128 ? (r >> 1) & 7 : r & 15; }); };
+  auto issue_v = [&](int slot) { issue(next_v, p.ldv, lds_base + (2 + slot) * TILE, [](int r) { return PITCH == 128 ? (r << 1) & 4 : (r & 3) << 2; }); };
+  if (ntiles > 0) { issue_k(0); issue_v(0); }
+
+  // what the end needs is asked for now: the gains go behind the tiles, a wavefront of the second map keeps lambda
+  float* const gains = (float*)(lds + 4 * TILE);
+  for (int at = tid; at < w; at += 64 * NW) gains[at] = p.gain ? p.gain[at] : 1.f;
+  const int head = hk * p.group + hg;
+  const float lam = p.lambda[head];
 
   // ---- queries: B operand of the score product
-  const bf16* const qrow = (const bf16*)p.q + ((size_t)b * p.l + i) * p.ldq + (size_t)(hk * p.group + hg) * w;
-  bf16x8 qf[MAPS][NC];
+  const bf16* const qrow = (const bf16*)p.q + ((size_t)b * p.l + i) * p.ldq + (size_t)(hk * p.group + hg) * w + map * d;
+  bf16x8 qf[NC];
 #pragma unroll
-  for (int m = 0; m < MAPS; ++m)
+  for (int c = 0; c < NC; ++c) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) qf[m][c][e] = (bf16)0.f;
-      if (16 * c + 8 * half < d) qf[m][c] = *(const bf16x8*)(qrow + (map0 + m) * d + 16 * c + 8 * half);
-    }
-  f32x16 o[MAPS][NC];
-  float m_ref[MAPS], neg[MAPS], l_run[MAPS];
-#pragma unroll
-  for (int m = 0; m < MAPS; ++m) {
-    m_ref[m] = -INFINITY; neg[m] = 0.f; l_run[m] = 0.f;
-#pragma unroll
-    for (int t = 0; t < NC; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[m][t][r] = 0.f;
+    for (int e = 0; e < 8; ++e) qf[c][e] = (bf16)0.f;
+    if (16 * c + 8 * half < d) qf[c] = *(const bf16x8*)(qrow + 16 * c + 8 * half);
   }
-  // fragment offsets in a tile: K row l32, 16-byte chunk map * d / 8 + 2 c + half at its swizzled place
-  const int k_swz = PITCH == 128 ? (l32 >> 1) & 7 : l32 & 15;
-  // V: the 16 lanes of a group read four keys' 16 columns; lane x of a group addresses key x / 4, columns 4 (x % 4)
+  f32x16 o[NC], s[2];
+  bf16x8 pb[2][2];
+  float m_ref = -INFINITY, neg = __builtin_nanf(""), l_run = 0.f;
+#pragma unroll
+  for (int t = 0; t < NC; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { pb[1][0][e] = (bf16)0.f; pb[1][1][e] = (bf16)0.f; }
+
+  // fragments.  K: row l32 of block j, 16-byte chunk map * d / 8 + 2 c + half at its swizzled place
+  const int k_swz = PITCH == 128 ? (l32 >> 1) & 7 : l32 & 15, k_chunk = map * (d >> 3) + half;
+  unsigned k_at[NC];                                           // in tile 0 or 1 of k (of which the last step read)
+#pragma unroll
+  for (int c = 0; c < NC; ++c) k_at[c] = (my_block * 64 + l32) * PITCH + (((k_chunk + 2 * c) ^ k_swz) << 4);
+  auto k_frag = [&](int j, int c) __attribute__((always_inline)) { return *(const bf16x8*)(lds + k_at[c] + j * 32 * PITCH); };
+  // V^T, n: tile of 32 columns n / 2, keys 16 (n % 2) .. of the block.  The 16 lanes of a group read four keys' 16 columns; lane x of a group addresses
+  // key x / 4, columns 4 (x % 4)
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
   const int x16 = lane & 15, v_row = 4 * half + (x16 >> 2), v_chunk = 2 * ((lane >> 4) & 1) + ((x16 & 3) >> 1);
   const int v_swz = PITCH == 128 ? (v_row << 1) & 4 : (v_row & 3) << 2;
-  const int v_base = v_row * PITCH + 8 * (x16 & 1);
-
-  auto block = [&](const char* Ks, int j, int kb, bool masked) {
-    const char* Vs = Ks + TILE;
-    f32x16 s[MAPS];
+  constexpr int VA = NC < 4 ? NC : 4;                          // tiles 4 .. 7 lie 256 bytes behind tiles 0 .. 3
+  unsigned v_at[VA];
 #pragma unroll
-    for (int m = 0; m < MAPS; ++m) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[m][r] = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const bf16x8 kf = *(const bf16x8*)(Ks + (j * 32 + l32) * PITCH + ((((map0 + m) * d8 + 2 * c + half) ^ k_swz) << 4));
-        s[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[m][c], s[m], 0, 0, 0);
-      }
-    }
-    if (masked) {
-#pragma unroll
-      for (int m = 0; m < MAPS; ++m)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (kb + 8 * (r >> 2) + 4 * half + (r & 3) >= limit) s[m][r] = -INFINITY;
-    }
-    bf16x8 pb[MAPS][2];
-    auto probs = [&](int m) {
-      float sum = 0.f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[m][r], p.scale_log2, neg[m]));
-        sum += e;
-        pb[m][r >> 3][r & 7] = (bf16)e;
-      }
-      return sum;
-    };
-    float sum[MAPS];
-    bool redo[MAPS], any = false;
-#pragma unroll
-    for (int m = 0; m < MAPS; ++m) {
-      sum[m] = probs(m);
-      redo[m] = !(sum[m] < kDiffBig) || m_ref[m] == -INFINITY;
-      any |= redo[m];
-    }
-    if (__builtin_amdgcn_ballot_w64(any) != 0) {
-#pragma unroll
-      for (int m = 0; m < MAPS; ++m) {
-        // only rows that asked for it (either half) move: what a row gives does not depend on the rows beside it
-        const float mine = redo[m] ? 1.f : 0.f;
-        const bool move = mine + other_half(mine, low) != 0.f;
-        float a = s[m][0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) a = fmaxf(a, s[m][r]);
-        a = fmaxf(a, other_half(a, low)) * p.scale_log2;
-        const float up = move ? fmaxf(m_ref[m], a) : m_ref[m];
-        const float keep = !move || m_ref[m] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_ref[m] - up);
-        m_ref[m] = up;
-        neg[m] = up == -INFINITY ? 0.f : -up;
-        l_run[m] *= keep;
-#pragma unroll
-        for (int t = 0; t < NC; ++t)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[m][t][r] *= keep;
-        sum[m] = probs(m);
-      }
-    }
-#pragma unroll
-    for (int m = 0; m < MAPS; ++m) l_run[m] += sum[m];
-#pragma unroll
-    for (int t = 0; t < NC; ++t)
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        typedef short s16x4 __attribute__((ext_vector_type(4)));
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        const char* at = Vs + (j * 32 + 16 * s2) * PITCH + v_base + (((4 * t + v_chunk) ^ v_swz) << 4);
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
-        const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * PITCH));
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int m = 0; m < MAPS; ++m) o[m][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[m][s2], o[m][t], 0, 0, 0);
-      }
+  for (int t = 0; t < VA; ++t) v_at[t] = 2 * TILE + (my_block * 64 + v_row) * PITCH + 8 * (x16 & 1) + (((4 * t + v_chunk) ^ v_swz) << 4);
+  auto v_frag = [&](int j, int n) __attribute__((always_inline)) {
+    const char* const at = lds + v_at[(n >> 1) % 4] + (n >> 3) * 256 + (32 * j + 16 * (n & 1)) * PITCH;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+    const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * PITCH));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-
-  for (int t = 0; t < ntiles; ++t) {
-    wait_vmcnt<0>();
-    __syncthreads();
-    if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1);
-    const char* const Ks = lds + (t & 1) * STAGE;
-#pragma unroll 1
-    for (int j = FEW ? my_block : 0; j < (FEW ? my_block + 1 : 2); ++j) {
-      const int kb = from + 64 * t + 32 * j;
-      if (kb < lim_last) block(Ks, j, kb, kb + 32 > lim_first);
-    }
-  }
-
-  float l_tot[MAPS];
+  const bf16x2 ones = {(bf16)1.f, (bf16)1.f};
+  // weights from registers r and r + 1 of the scores; returns the row's sum with them
+  auto weigh = [&](int x, int r, float sum) __attribute__((always_inline)) {
+    const bf16x2 e = {(bf16)__builtin_amdgcn_exp2f(fmaf(s[x][r], p.scale_log2, neg)), (bf16)__builtin_amdgcn_exp2f(fmaf(s[x][r + 1], p.scale_log2, neg))};
+    pb[x][r >> 3][r & 7] = e[0];
+    pb[x][r >> 3][(r & 7) + 1] = e[1];
+    return __builtin_amdgcn_fdot2_f32_bf16(e, ones, sum, false);
+  };
+  // A step, in one straight line: the scores of the next block, the products of the block before with its values, and between those MFMAs the weights of
+  // this block, x its place in its tile.  Fragments are asked for AHEAD MFMAs early.
+  auto step = [&](int x) __attribute__((always_inline)) {
+    constexpr int NM = 3 * NC, AHEAD = 3;
+    bf16x8 fr[AHEAD + 1];
+    auto fetch = [&](int g) { fr[g % (AHEAD + 1)] = g < NC ? k_frag(1 - x, g) : v_frag(1 - x, g - NC); };
 #pragma unroll
-  for (int m = 0; m < MAPS; ++m) l_tot[m] = l_run[m] + other_half(l_run[m], low);
-  float* const hand = (float*)lds;
-  constexpr int HAND = (16 * NC + 2) * 64;                     // a wavefront's sums, a register of all lanes at a time
-  if constexpr (FEW) {
-    // the second block's wavefronts hand theirs to the first's
-    __syncthreads();
-    float* const at = hand + map0 * HAND + lane;
-    if (my_block == 1) {
+    for (int g = 0; g < AHEAD; ++g) fetch(g);
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[1 - x][r] = 0.f;
+    unrolled<NM>([&](auto g_) __attribute__((always_inline)) {
+      constexpr int g = decltype(g_)::value;
+#pragma unroll
+      for (int e = (8 * g + NM - 1) / NM; e < (8 * (g + 1) + NM - 1) / NM; ++e) sum[e & 1] = weigh(x, 2 * e, sum[e & 1]);
+      if constexpr (g + AHEAD < NM) fetch(g + AHEAD);
+      const bf16x8& f = fr[g % (AHEAD + 1)];
+      if constexpr (g < NC) s[1 - x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[g], s[1 - x], 0, 0, 0);
+      else o[(g - NC) >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[1 - x][(g - NC) & 1], o[(g - NC) >> 1], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    return sum[0] + sum[1];
+  };
+  // first block of this wavefront (of 32 keys, two a tile) of which a row does not see all
+  auto masked = [&](int t, int x) { return from + KEYS * t + 64 * my_block + 32 * x + 32 > lim_first; };
+  auto mask = [&](int t, int x) __attribute__((always_inline)) {
+    if (masked(t, x)) {
+      const int kb = from + KEYS * t + 64 * my_block + 32 * x + 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (kb + 8 * (r >> 2) + (r & 3) >= limit) s[x][r] = -INFINITY;
+    }
+  };
+  // takes a block's sum of weights in, or raises the reference first.  Without a reference the weights are NaN.  Only rows that ask for it (either half)
+  // move: what a row gives does not depend on the rows beside it
+  auto settle = [&](int x, float sum) __attribute__((always_inline)) {
+    const bool redo = !(sum < kDiffBig);
+    if (__builtin_amdgcn_ballot_w64(redo) != 0) {
+      const float mine = redo ? 1.f : 0.f;
+      const bool move = mine + other_half(mine, low) != 0.f;
+      float a = s[x][0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) a = fmaxf(a, s[x][r]);
+      a = fmaxf(a, other_half(a, low)) * p.scale_log2;
+      const float up = move ? fmaxf(m_ref, a) : m_ref;
+      const float keep = !move || m_ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_ref - up);
+      m_ref = up;
+      neg = up == -INFINITY ? 0.f : -up;
+      l_run *= keep;
 #pragma unroll
       for (int t = 0; t < NC; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) at[(16 * t + r) * 64] = o[0][t][r];
-      at[16 * NC * 64] = m_ref[0];
-      at[(16 * NC + 1) * 64] = l_tot[0];
+        for (int r = 0; r < 16; ++r) o[t][r] *= keep;
+      sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) sum = weigh(x, r, sum);
+      if (up == -INFINITY) neg = __builtin_nanf("");
+    }
+    l_run += sum;
+  };
+
+  if (ntiles > 0) {
+    // in front of the first block the weights are zero; what they are multiplied with must not be NaN
+    for (int at = tid * 16; at < TILE; at += 16 * 64 * NW) *(f32x4*)(lds + 3 * TILE + at) = f32x4{0.f, 0.f, 0.f, 0.f};
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (ntiles > 1) issue_k(1);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(0, c), qf[c], s[0], 0, 0, 0);
+#pragma unroll
+    for (int t = 0; t < VA; ++t) v_at[t] ^= TILE;
+#pragma unroll 1
+    for (int t = 0; t < ntiles; ++t) {
+      mask(t, 0);
+      settle(0, step(0));                                      // k: tile t, v: tile t - 1
+#pragma unroll
+      for (int c = 0; c < NC; ++c) k_at[c] ^= TILE;
+#pragma unroll
+      for (int c = 0; c < VA; ++c) v_at[c] ^= TILE;
+      // tile t + 1 of k and tile t of v have landed, and everybody is done with tile t of k and tile t - 1 of v
+      wait_vmcnt<0>();
+      __syncthreads();
+      if (t + 2 < ntiles) issue_k(t & 1);
+      if (t + 1 < ntiles) issue_v((t + 1) & 1);
+      mask(t, 1);
+      settle(1, step(1));                                      // k: tile t + 1 (behind the last tile: whatever lies there, not used), v: tile t
+    }
+#pragma unroll
+    for (int n = 0; n < 2 * NC; ++n) o[n >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(1, n), pb[1][n & 1], o[n >> 1], 0, 0, 0);
+  }
+
+  l_run += other_half(l_run, low);
+  // sums change hands in LDS, four registers of all lanes at a time
+  auto quad = [&](int t, int q4) { return f32x4{o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]}; };
+  if constexpr (WB > 1) {
+    // the other blocks' wavefronts hand theirs to the first's
+    constexpr int HAND = (4 * NC + 1) * 64;                    // quads
+    static_assert((WB - 1) * 2 * WR * HAND * 16 <= 4 * TILE, "the sums");
+    f32x4* const mine = (f32x4*)lds + (row_wave * 2 + map) * (WB - 1) * HAND + lane;
+    __syncthreads();
+    if (my_block > 0) {
+      f32x4* const at = mine + (my_block - 1) * HAND;
+#pragma unroll
+      for (int t = 0; t < NC; ++t)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) at[(4 * t + q4) * 64] = quad(t, q4);
+      at[4 * NC * 64] = f32x4{m_ref, l_run, 0.f, 0.f};
     }
     __syncthreads();
     if (my_block == 0) {
-      const float other = at[16 * NC * 64], up = fmaxf(m_ref[0], other), ref = up == -INFINITY ? 0.f : up;
-      const float f0 = __builtin_amdgcn_exp2f(m_ref[0] - ref), f1 = __builtin_amdgcn_exp2f(other - ref);
-      m_ref[0] = up;
-      l_tot[0] = l_tot[0] * f0 + at[(16 * NC + 1) * 64] * f1;
-#pragma unroll
-      for (int t = 0; t < NC; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[0][t][r] = o[0][t][r] * f0 + at[(16 * t + r) * 64] * f1;
-    }
-  }
-  if (p.splits > 1) {
-    if ((!FEW || my_block == 0) && row < p.rows) {
-      float* const rec = p.partial + diff_record(p, bh, row, split);
-#pragma unroll
-      for (int m = 0; m < MAPS; ++m) {
+#pragma unroll 1
+      for (int g = 0; g < WB - 1; ++g) {
+        const f32x4* const at = mine + g * HAND;
+        const f32x4 ml = at[4 * NC * 64];
+        const float up = fmaxf(m_ref, ml[0]), ref = up == -INFINITY ? 0.f : up;
+        const float f0 = __builtin_amdgcn_exp2f(m_ref - ref), f1 = __builtin_amdgcn_exp2f(ml[0] - ref);
+        m_ref = up;
+        l_run = l_run * f0 + ml[1] * f1;
 #pragma unroll
         for (int t = 0; t < NC; ++t)
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
-            const int col = 32 * t + 8 * q4 + 4 * half;
-            if (col < w) *(f32x4*)(rec + (map0 + m) * w + col) = f32x4{o[m][t][4 * q4], o[m][t][4 * q4 + 1], o[m][t][4 * q4 + 2], o[m][t][4 * q4 + 3]};
+            const f32x4 x = at[(4 * t + q4) * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[t][4 * q4 + e] = o[t][4 * q4 + e] * f0 + x[e] * f1;
           }
-        if (low) { rec[2 * w + 2 * (map0 + m)] = m_ref[m]; rec[2 * w + 2 * (map0 + m) + 1] = l_tot[m]; }
       }
     }
-    return;
   }
-  const int head = hk * p.group + hg;
-  const float lam = p.lambda[head];
-  f32x16 res[NC];
-  if constexpr (FEW) {
-    // the second map's wavefront hands lambda o2 / l2 to the first's
-    __syncthreads();
-    if (wave == 1) {
-      const float f2 = lam * inverse_or_zero(l_tot[0]);
+  if (p.splits > 1) {
+    if (my_block == 0 && row < p.rows) {
+      float* const rec = p.partial + diff_record(p, bh, row, split);
 #pragma unroll
       for (int t = 0; t < NC; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) hand[(16 * t + r) * 64 + lane] = o[0][t][r] * f2;
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const int col = 32 * t + 8 * q4 + 4 * half;
+          if (col < w) *(f32x4*)(rec + map * w + col) = quad(t, q4);
+        }
+      if (low) { rec[2 * w + 2 * map] = m_ref; rec[2 * w + 2 * map + 1] = l_run; }
     }
-    __syncthreads();
-    if (wave > 0) return;
-    const float f1 = inverse_or_zero(l_tot[0]);
-#pragma unroll
-    for (int t = 0; t < NC; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) res[t][r] = o[0][t][r] * f1 - hand[(16 * t + r) * 64 + lane];
-  } else {
-    const float f1 = inverse_or_zero(l_tot[0]), f2 = lam * inverse_or_zero(l_tot[MAPS - 1]);
-#pragma unroll
-    for (int t = 0; t < NC; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) res[t][r] = o[0][t][r] * f1 - o[MAPS - 1][t][r] * f2;
+    return;
   }
+  // the second map's wavefront hands lambda o2 / l2 to the first's
+  static_assert(WR * 16 * NC * 64 * 4 <= 4 * TILE, "a map's results");
+  f32x4* const at = (f32x4*)lds + row_wave * (4 * NC * 64) + lane;
+  __syncthreads();
+  if (map == 1 && my_block == 0) {
+    const float f2 = lam * inverse_or_zero(l_run);
+#pragma unroll
+    for (int t = 0; t < NC; ++t)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) at[(4 * t + q4) * 64] = quad(t, q4) * f2;
+  }
+  __syncthreads();
+  if (map == 1 || my_block > 0) return;
+  const float f1 = inverse_or_zero(l_run);
   float sq = 0.f;
 #pragma unroll
   for (int t = 0; t < NC; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sq = fmaf(res[t][r], res[t][r], sq);     // columns behind 2 d are zero
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const f32x4 x = quad(t, q4) * f1 - at[(4 * t + q4) * 64];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[t][4 * q4 + e] = x[e];
+        sq = fmaf(x[e], x[e], sq);                             // columns behind 2 d are zero
+      }
+    }
   sq += other_half(sq, low);
   const float r0 = p.gain ? p.out_scale * rsqrtf(sq / (float)w + p.eps) : p.out_scale;
   if (row >= p.rows) return;
@@ -470,9 +537,10 @@ __global__ __launch_bounds__(256, NC <= 2 ? 3 : NC <= 4 ? 2 : 1) void k_diff_mfm
     for (int q4 = 0; q4 < 4; ++q4) {
       const int col = 32 * t + 8 * q4 + 4 * half;
       if (col >= w) continue;
+      const f32x4 g4 = *(const f32x4*)(gains + col);
       bf16x4 v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (bf16)(res[t][4 * q4 + e] * r0 * (p.gain ? p.gain[col + e] : 1.f));
+      for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[t][4 * q4 + e] * r0 * g4[e]);
       *(bf16x4*)(out + col) = v;
     }
 }
@@ -537,15 +605,18 @@ __global__ __launch_bounds__(256) void k_diff_join(DiffParams p) {
   *(typename Quad<T>::type*)((T*)p.out + ((size_t)b * p.l + query) * p.ldo + (size_t)head * w + 4 * lane) = res;
 }
 
-// How a call is cut up: rows a workgroup takes, and over how many workgroups the keys of a row are shared out where the rows leave the chip idle (at
-// least 256 keys each)
-struct DiffPlan { bool few; int rows_a_tile, tiles, splits; };
+// How a call is cut up: rows a workgroup takes, and over how many workgroups the keys of a row are shared out.
+// Rows, bf16: the largest tile that gives 150 workgroups.  A larger tile reads keys and values less often, and its wavefronts hide each other's waits; too few
+// leave CUs idle.  us at 128 / 64 / 32 rows: 2304 x 2304, 5 heads of 2 x 64, two samples 54 (180 workgroups) / 58 / 86, one sample 52 (90) / 41 / 57;
+// 1024 x 1024, 5 heads of 2 x 64 29 (40) / 23 (80) / 19; 3000 x 3000, 8 heads of 2 x 128 on 2 129 (188) / 168 / 248, 4 heads on 4 at 1511 70 (48) / 49 / 49.
+// Keys: shared out where the tiles leave the chip idle, at least 128 each.  us with 1 / 2 / 4 / 8 / .. shares: 64 tiles of 8192 keys 79 / 50 / 33 / 40 / 53; 16 tiles
+// 79 / 47 / 29 / 21 / 19 / 28; 80 tiles of 2048 keys 26 / 24 / 30; 160 tiles of 1024 keys 19 / 33: the sums' way through memory costs more than it brings.
+struct DiffPlan { int rows_a_tile, tiles, splits; };
 static DiffPlan diff_plan(int dtype, long long bh, int rows, int lk) {
   DiffPlan a{};
-  a.few = dtype == AD_BF16 && bh * ((rows + 127) / 128) <= 256;
-  a.rows_a_tile = dtype == AD_F32 ? 16 : a.few ? 32 : 128;
+  a.rows_a_tile = dtype == AD_F32 ? 16 : bh * ((rows + 127) / 128) >= 150 ? 128 : bh * ((rows + 63) / 64) >= 150 ? 64 : 32;
   a.tiles = (rows + a.rows_a_tile - 1) / a.rows_a_tile;
-  const long long tiles = bh * a.tiles, want = (512 + tiles - 1) / tiles, most = (lk + 255) / 256;
+  const long long want = 256 / (bh * a.tiles), most = (lk + 127) / 128;
   a.splits = (int)std::max(1LL, std::min(std::min(want, most), (long long)kDiffMaxSplits));
   return a;
 }
@@ -560,7 +631,7 @@ static size_t diff_partial_bytes(long long bh, long long rows, int splits, int d
 template <typename K>
 static ad_status launch_diff(K kern, int threads, int lds_bytes, std::atomic<bool>& attr_set, unsigned blocks, const DiffParams& p, hipStream_t s) {
   if (lds_bytes > 65536 && !attr_set) {
-    AD_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes));
+    AD_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
     attr_set = true;
   }
   hipLaunchKernelGGL(kern, dim3(blocks), dim3(threads), lds_bytes, s, p);
@@ -569,23 +640,29 @@ static ad_status launch_diff(K kern, int threads, int lds_bytes, std::atomic<boo
 }
 
 template <int DT>
-static ad_status run_diff_generic(const DiffParams& p, unsigned blocks, hipStream_t s) {
+static ad_status run_diff_f32(const DiffParams& p, unsigned blocks, hipStream_t s) {
   static std::atomic<bool> attr_set{false};
-  return launch_diff(k_diff_generic<float, DT>, 512, 8 * 16 * (64 * ((2 * DT + 3) / 4) + 4) * 4, attr_set, blocks, p, s);
+  return launch_diff(k_diff_f32<DT>, 256, 4 * 16 * (64 * ((2 * DT + 3) / 4) + 4) * 4, attr_set, blocks, p, s);
 }
 
+template <int NC, int WR, int WB, int OCC>
+static ad_status run_diff_waves(const DiffParams& p, unsigned blocks, hipStream_t s) {
+  static std::atomic<bool> attr_set{false};
+  return launch_diff(k_diff_mfma<NC, WR, WB, OCC>, 128 * WR * WB, 4 * 64 * WB * diff_pitch(NC) + 8 * p.d, attr_set, blocks, p, s);
+}
+// OCC: wavefronts per SIMD that the register budget is set for; heads wider than 96 have a CU's LDS for one workgroup
 template <int NC>
-static ad_status run_diff_mfma(const DiffParams& p, bool few, unsigned blocks, hipStream_t s) {
-  constexpr int lds_bytes = 2 * 2 * 64 * diff_pitch(NC);
-  static_assert(2 * (16 * NC + 2) * 64 * 4 <= lds_bytes, "the sums of two wavefronts");
-  static std::atomic<bool> set_few{false}, set_many{false};
-  return few ? launch_diff(k_diff_mfma<NC, true>, 256, lds_bytes, set_few, blocks, p, s) : launch_diff(k_diff_mfma<NC, false>, 256, lds_bytes, set_many, blocks, p, s);
+static ad_status run_diff_mfma(const DiffParams& p, const DiffPlan& plan, unsigned blocks, hipStream_t s) {
+  constexpr int OCC = NC <= 2 ? 4 : 2, OCC_FEW = NC > 6 ? 1 : OCC;
+  if (plan.rows_a_tile == 128) return run_diff_waves<NC, 4, 1, OCC>(p, blocks, s);
+  if (plan.rows_a_tile == 64) return run_diff_waves<NC, 2, 1, OCC_FEW>(p, blocks, s);
+  return run_diff_waves<NC, 1, NC <= 4 ? 2 : 1, OCC_FEW>(p, blocks, s);
 }
 
 static ad_status run_diff(int dtype, DiffParams p, const DiffPlan& plan, int batch, hipStream_t s) {
   p.tiles = plan.tiles;
   p.splits = plan.splits;
-  const int step = dtype == AD_BF16 ? 64 : 16;
+  const int step = dtype == AD_BF16 ? 128 : 16;
   p.split_keys = ((p.lk + p.splits - 1) / p.splits + step - 1) / step * step;
   p.div_tiles = make_fastdiv((unsigned)p.tiles);
   p.div_splits = make_fastdiv((unsigned)p.splits);
@@ -593,17 +670,17 @@ static ad_status run_diff(int dtype, DiffParams p, const DiffPlan& plan, int bat
   const int chunks = (p.d + 15) / 16;
   ad_status st;
   if (dtype == AD_BF16) {
-    if (chunks <= 2) st = run_diff_mfma<2>(p, plan.few, blocks, s);
-    else if (chunks == 3) st = run_diff_mfma<3>(p, plan.few, blocks, s);
-    else if (chunks == 4) st = run_diff_mfma<4>(p, plan.few, blocks, s);
-    else if (chunks == 5) st = run_diff_mfma<5>(p, plan.few, blocks, s);
-    else if (chunks == 6) st = run_diff_mfma<6>(p, plan.few, blocks, s);
-    else st = run_diff_mfma<8>(p, plan.few, blocks, s);
+    if (chunks <= 2) st = run_diff_mfma<2>(p, plan, blocks, s);
+    else if (chunks == 3) st = run_diff_mfma<3>(p, plan, blocks, s);
+    else if (chunks == 4) st = run_diff_mfma<4>(p, plan, blocks, s);
+    else if (chunks == 5) st = run_diff_mfma<5>(p, plan, blocks, s);
+    else if (chunks == 6) st = run_diff_mfma<6>(p, plan, blocks, s);
+    else st = run_diff_mfma<8>(p, plan, blocks, s);
   } else {
-    if (chunks <= 1) st = run_diff_generic<1>(p, blocks, s);
-    else if (chunks == 2) st = run_diff_generic<2>(p, blocks, s);
-    else if (chunks <= 4) st = run_diff_generic<4>(p, blocks, s);
-    else st = run_diff_generic<8>(p, blocks, s);
+    if (chunks <= 1) st = run_diff_f32<1>(p, blocks, s);
+    else if (chunks == 2) st = run_diff_f32<2>(p, blocks, s);
+    else if (chunks <= 4) st = run_diff_f32<4>(p, blocks, s);
+    else st = run_diff_f32<8>(p, blocks, s);
   }
   if (st != AD_OK || p.splits <= 1) return st;
   const unsigned total = (unsigned)(batch * p.kv_heads) * (unsigned)p.rows;
