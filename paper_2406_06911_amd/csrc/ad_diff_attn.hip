@@ -13,6 +13,10 @@
 namespace ad {
 
 constexpr float kLog2e = 1.44269504088896341f;
+// The exponential's reference need not be the running maximum: any value near it gives the same quotient.  It is the exact maximum of the first block
+// of keys that a row sees, and is raised (and what has been summed rescaled) when a block's sum of weights reaches 2^24, so the steady state computes no
+// maximum.  A row sees a prefix of its keys, so where it sees any of a share, it sees the first.
+constexpr float kDiffBig = 16777216.f;
 constexpr int kDiffMaxSplits = 64;   // shares of the keys: a lane each when they are joined
 
 struct DiffParams {
@@ -66,7 +70,7 @@ __global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p)
   const int i = live ? (int)fast_div((unsigned)row, p.div_group) : 0, hg = live ? row - i * p.group : 0;
   // keys that this lane's row sees: 0 .. limit - 1; the workgroup's are those of its last row
   auto limit_of = [&](int query) { return p.causal ? min(max(query + len - p.l + 1, 0), len) : len; };
-  const int limit = live ? limit_of(i) : 0;
+  const int limit = live ? limit_of(i) : len, limit_first = limit_of((int)fast_div(tile * 16u, p.div_group));
   const int last = min((int)tile * 16 + 15, p.rows - 1);
   const int from = split * p.split_keys, to = min(from + p.split_keys, limit_of((int)fast_div((unsigned)last, p.div_group)));
 
@@ -81,7 +85,7 @@ __global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p)
     for (int c = 0; c < DT; ++c) qf[m][c] = live && 16 * c + 4 * g < d ? *(const f32x4*)(qrow + m * d + 16 * c + 4 * g) : zero;
 
   f32x4 o[2][VT][4];
-  float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+  float top[2] = {-INFINITY, -INFINITY}, neg[2] = {__builtin_nanf(""), __builtin_nanf("")}, sum[2] = {0.f, 0.f};
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -101,52 +105,79 @@ __global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p)
     for (int e = 0; e < 4; ++e) gain[t][e] = p.gain && 64 * t + c0 < w ? p.gain[64 * t + c0 + e] : 1.f;
 
   f32x4 kf[2][DT], vf[VT][4];                      // of a block: k [map][chunk of row r16], v [run of 64 columns][key 4 g + r]
-  auto fetch_k = [&](int key0) {
+  // No load is left out, so that the loop can wait for just the ones it needs: columns behind the head read its first ones (q is zero there, and what such
+  // columns of v give is dropped), keys behind the last read the last (their weight is zero)
+  int col_k[DT], col_v[VT];
+#pragma unroll
+  for (int c = 0; c < DT; ++c) col_k[c] = 16 * c + 4 * g < d ? 16 * c + 4 * g : 0;
+#pragma unroll
+  for (int t = 0; t < VT; ++t) col_v[t] = 64 * t + 4 * r16 < w ? 64 * t + 4 * r16 : 0;
+  auto fetch_k = [&](int key0) __attribute__((always_inline)) {
     const float* const krow = kbase + (size_t)min(key0 + r16, len - 1) * p.ldk;
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int c = 0; c < DT; ++c) kf[m][c] = 16 * c + 4 * g < d ? *(const f32x4*)(krow + m * d + 16 * c + 4 * g) : zero;
+      for (int c = 0; c < DT; ++c) kf[m][c] = *(const f32x4*)(krow + m * d + col_k[c]);
   };
-  auto fetch_v = [&](int key0) {
+  auto fetch_v = [&](int key0) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int key = key0 + 4 * g + r;
-      const float* const vrow = vbase + (size_t)min(key, len - 1) * p.ldv;
+      const float* const vrow = vbase + (size_t)min(key0 + 4 * g + r, len - 1) * p.ldv;
 #pragma unroll
-      for (int t = 0; t < VT; ++t) vf[t][r] = key < len && 64 * t + 4 * r16 < w ? *(const f32x4*)(vrow + 64 * t + 4 * r16) : zero;
+      for (int t = 0; t < VT; ++t) vf[t][r] = *(const f32x4*)(vrow + col_v[t]);
     }
   };
   if (from + 16 * wave < to) { fetch_k(from + 16 * wave); fetch_v(from + 16 * wave); }
   for (int key0 = from + 16 * wave; key0 < to; key0 += 16 * NW) {
     const int next = key0 + 16 * NW;
-    f32x4 s[2] = {zero, zero};
+    f32x4 s[2] = {zero, zero}, s_odd[2] = {zero, zero};   // four chains in turn: a product waits for the one in front of it in its chain
 #pragma unroll
     for (int c = 0; c < DT; ++c)
 #pragma unroll
-      for (int m = 0; m < 2; ++m) Mma16<float>::run(kf[m][c], qf[m][c], s[m]);
-    if (next < to) fetch_k(next);
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          f32x4& to_sum = e & 1 ? s_odd[m] : s[m];
+          to_sum = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[m][c][e], qf[m][c][e], to_sum, 0, 0, 0);
+        }
+    s[0] += s_odd[0];
+    s[1] += s_odd[1];
+    fetch_k(min(next, to - 1));
+    f32x4 pr[2];
+    float add[2];
+    auto weigh = [&](int m) __attribute__((always_inline)) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) pr[m][r] = __builtin_amdgcn_exp2f(fmaf(s[m][r], p.scale_log2, neg[m]));
+      add[m] = (pr[m][0] + pr[m][1]) + (pr[m][2] + pr[m][3]);
+    };
+    if (key0 + 16 > limit_first) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (key0 + 4 * g + r >= limit) s[m][r] = -INFINITY;
+    }
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      float most = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[m][r] = key0 + 4 * g + r < limit ? s[m][r] * p.scale_log2 : -INFINITY;
-        most = fmaxf(most, s[m][r]);
-      }
-      const float up = fmaxf(top[m], group_max(most));
-      const float keep = up == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[m] - up), ref = up == -INFINITY ? 0.f : up;
-      top[m] = up;
-      float add = 0.f;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) { s[m][r] = __builtin_amdgcn_exp2f(s[m][r] - ref); add += s[m][r]; }
-      sum[m] = sum[m] * keep + add;              // of this lane's keys; the four groups are added at the end
-      if (__builtin_amdgcn_ballot_w64(keep != 1.f) != 0) {
+      weigh(m);
+      // without a reference the weights are NaN; only rows that ask for a higher one (any of their four lanes) move
+      const bool redo = !(add[m] < kDiffBig);
+      if (__builtin_amdgcn_ballot_w64(redo) != 0) {
+        const bool move = group_max(redo ? 1.f : 0.f) != 0.f;
+        const float most = group_max(fmaxf(fmaxf(s[m][0], s[m][1]), fmaxf(s[m][2], s[m][3]))) * p.scale_log2;
+        const float up = move ? fmaxf(top[m], most) : top[m];
+        const float keep = !move || top[m] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[m] - up);
+        top[m] = up;
+        neg[m] = up == -INFINITY ? 0.f : -up;
+        sum[m] *= keep;
 #pragma unroll
         for (int t = 0; t < VT; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[m][t][e] *= keep;
+        weigh(m);
+        if (up == -INFINITY) neg[m] = __builtin_nanf("");
       }
+      sum[m] += add[m];                          // of this lane's keys; the four groups are added at the end
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -155,8 +186,8 @@ __global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int m = 0; m < 2; ++m) o[m][t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[t][r][e], s[m][r], o[m][t][e], 0, 0, 0);
-    if (next < to) fetch_v(next);
+          for (int m = 0; m < 2; ++m) o[m][t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[t][r][e], pr[m][r], o[m][t][e], 0, 0, 0);
+    fetch_v(min(next, to - 1));
   }
 
   // the wavefronts' sums meet in LDS, a map at a time; 16 threads take a row, columns 4 c .. 4 c + 3 of every run of 64
@@ -205,8 +236,8 @@ __global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p)
   const float f1 = inverse_or_zero(sums[0]), f2 = lam * inverse_or_zero(sums[1]);
   float sq = 0.f;
 #pragma unroll
-  for (int t = 0; t < VT; ++t) {                               // columns behind 2 d are zero
-    acc[0][t] = acc[0][t] * f1 - acc[1][t] * f2;
+  for (int t = 0; t < VT; ++t) {
+    acc[0][t] = 64 * t + c0 < w ? acc[0][t] * f1 - acc[1][t] * f2 : zero;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sq = fmaf(acc[0][t][e], acc[0][t][e], sq);
   }
@@ -235,10 +266,6 @@ __global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p)
 // A step of 32 keys is one straight line of MFMAs, the scores of the next block and the products of the block before, with the exponentials of this
 // block between them; the order is pinned, left alone the exponentials gather behind the MFMAs.  So k runs a tile ahead of v, and a barrier every two steps is enough.
 //
-// The exponential's reference need not be the running maximum: any value near it gives the same quotient.  It is the exact maximum of the first 32 keys
-// that a row sees, and is raised (and what has been summed rescaled) when a block's sum of weights reaches 2^24, so the steady state computes no
-// maximum.  A row sees a prefix of its keys, so where it sees any of a share, it sees the first.
-//
 // Probabilities are rounded to bf16 for the product with v, and the row's sum is of the rounded ones (half the instructions of a sum in front of the
 // rounding; the weights then add up to 1); scores, sums and references are fp32; q is not scaled in front of the product (a rounding less).
 //
@@ -254,7 +281,6 @@ template <int N, typename F> __device__ __forceinline__ void unrolled(F&& f) {
   }
 }
 constexpr int diff_pitch(int nc) { return nc <= 2 ? 128 : nc <= 4 ? 256 : 512; }
-constexpr float kDiffBig = 16777216.f;   // 2^24
 
 template <int NC, int WR, int WB, int OCC>
 __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) {
