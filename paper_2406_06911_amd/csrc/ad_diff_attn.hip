@@ -571,6 +571,152 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
     }
 }
 
+// =================================================================================================
+// bf16, up to 96 keys and heads of 2 x 64 (image tokens against a text): all keys and values of a head lie in LDS, a wavefront takes 32 rows and holds the
+// scores of both maps in registers.  So the weights of both are known before the product with v, their difference is rounded once, and one product
+// does for both maps (8 d operations a pair instead of 12 d).  Bound by the chain load - scores - softmax - product - store and its vector instructions (about
+// 650 for 32 rows of 77 keys, both maps; masks only in blocks where a row does not see all: 982 with them everywhere, 15.6 us).
+// 2 x 9216 x 77, 5 heads of 2 x 32 (24 MB): 12.4 us, the kernel above 14.9; 2 x 36864 x 77 35 us, 2.7 TB/s.
+// =================================================================================================
+template <int NC, int NB>
+__global__ __launch_bounds__(256, NC <= 2 ? 3 : 2) void k_diff_short(DiffParams p) {
+  constexpr int PITCH = diff_pitch(NC), CPR = PITCH / 16, TILE = NB * 32 * PITCH, LPT = TILE / 4096;
+  extern __shared__ __attribute__((aligned(128))) char lds[];      // k, v
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const bool low = half == 0;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned vid = xcd_remap(blockIdx.x, gridDim.x);
+  const unsigned bh = fast_div(vid, p.div_tiles), tile = vid - bh * p.tiles;
+  const unsigned b = fast_div(bh, p.div_kv), hk = bh - b * p.kv_heads;
+  const int d = p.d, w = 2 * d;
+  const int len = __builtin_amdgcn_readfirstlane(p.key_lens ? min(max(p.key_lens[b], 0), p.lk) : p.lk);
+  const int row = tile * 128 + wave * 32 + l32, rowc = min(row, p.rows - 1);
+  const int i = (int)fast_div((unsigned)rowc, p.div_group), head = hk * p.group + rowc - i * p.group;
+  auto limit_of = [&](int query) { return p.causal ? min(max(query + len - p.l + 1, 0), len) : len; };
+  const int limit = limit_of(i), lim_first = limit_of((int)fast_div((unsigned)min((int)tile * 128 + wave * 32, p.rows - 1), p.div_group));
+
+  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds + wave * 1024u;
+  auto load = [&](const void* base, int ld, unsigned at, auto swizzle) __attribute__((always_inline)) {
+    // no key: nothing lies in range
+    u32x4 rsrc = make_rsrc_words((const bf16*)base + (size_t)b * p.lk * ld + (size_t)hk * w, len > 0 ? (unsigned)((len - 1) * ld + w) * 2u : 0u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rsrc[e] = __builtin_amdgcn_readfirstlane(rsrc[e]);
+#pragma unroll
+    for (int x = 0; x < LPT; ++x) {
+      const int id = (x * 4 + wave) * 64 + lane, r = id / CPR, c = (id % CPR) ^ swizzle(r);
+      dma_load16(rsrc, c * 8 < w && r < len ? (unsigned)(r * ld) * 2u + c * 16u : kOob, 0u, at + x * 4096u);
+    }
+  };
+  load(p.k, p.ldk, lds_base, [](int r) { return PITCH == 128 ? (r >> 1) & 7 : r & 15; });
+  load(p.v, p.ldv, lds_base + TILE, [](int r) { return PITCH == 128 ? (r << 1) & 4 : (r & 3) << 2; });
+  const bf16* const qrow = (const bf16*)p.q + ((size_t)b * p.l + i) * p.ldq + (size_t)head * w;
+  bf16x8 qf[2][NC];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qf[m][c][e] = (bf16)0.f;
+      if (16 * c + 8 * half < d) qf[m][c] = *(const bf16x8*)(qrow + m * d + 16 * c + 8 * half);
+    }
+  const float lam = p.lambda[head];
+  float* const gains = (float*)(lds + 2 * TILE);
+  if (tid < w) gains[tid] = p.gain ? p.gain[tid] : 1.f;
+  wait_vmcnt<0>();
+  __syncthreads();
+
+  f32x16 s[2][NB];
+  const int k_swz = PITCH == 128 ? (l32 >> 1) & 7 : l32 & 15;
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[m][j][r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const bf16x8 f = *(const bf16x8*)(lds + (32 * j + l32) * PITCH + (((m * (d >> 3) + 2 * c + half) ^ k_swz) << 4));
+        s[m][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[m][c], s[m][j], 0, 0, 0);
+      }
+    }
+  // weights of a map: exponentials relative to the row's maximum, and what they are multiplied with
+  float factor[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      if (32 * j + 32 > lim_first) {
+        const int seen = limit - 32 * j - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r >> 2) + (r & 3) >= seen) s[m][j][r] = -INFINITY;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) most = fmaxf(most, s[m][j][r]);
+    }
+    most = fmaxf(most, other_half(most, low)) * p.scale_log2;
+    const float neg = most == -INFINITY ? 0.f : -most;
+    f32x4 sums = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[m][j][r] = __builtin_amdgcn_exp2f(fmaf(s[m][j][r], p.scale_log2, neg));
+        sums[r & 3] += s[m][j][r];
+      }
+    const float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    factor[m] = inverse_or_zero(sum + other_half(sum, low));
+  }
+  factor[1] *= lam;
+
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  const int x16 = lane & 15, v_row = 4 * half + (x16 >> 2), v_chunk = 2 * ((lane >> 4) & 1) + ((x16 & 3) >> 1);
+  const int v_swz = PITCH == 128 ? (v_row << 1) & 4 : (v_row & 3) << 2;
+  const char* const v_at = lds + TILE + v_row * PITCH + 8 * (x16 & 1);
+  f32x16 o[NC];
+#pragma unroll
+  for (int t = 0; t < NC; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      bf16x8 pb;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pb[e] = (bf16)fmaf(s[0][j][8 * s2 + e], factor[0], -(s[1][j][8 * s2 + e] * factor[1]));
+#pragma unroll
+      for (int t = 0; t < NC; ++t) {
+        const char* const at = v_at + (32 * j + 16 * s2) * PITCH + (((4 * t + v_chunk) ^ v_swz) << 4);
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+        const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * PITCH));
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7)), pb, o[t], 0, 0, 0);
+      }
+    }
+  float sq = 0.f;
+#pragma unroll
+  for (int t = 0; t < NC; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sq = fmaf(o[t][r], o[t][r], sq);      // columns behind 2 d are zero
+  sq += other_half(sq, low);
+  const float r0 = p.gain ? p.out_scale * rsqrtf(sq / (float)w + p.eps) : p.out_scale;
+  if (row >= p.rows) return;
+  bf16* const out = (bf16*)p.out + ((size_t)b * p.l + i) * p.ldo + (size_t)head * w;
+#pragma unroll
+  for (int t = 0; t < NC; ++t)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const int col = 32 * t + 8 * q4 + 4 * half;
+      if (col >= w) continue;
+      const f32x4 g4 = *(const f32x4*)(gains + col);
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[t][4 * q4 + e] * r0 * g4[e]);
+      *(bf16x4*)(out + col) = v;
+    }
+}
+
 // Joins the shares of the keys, in their order.  A workgroup a row: the shares' references and sums give one factor each, then a thread has four
 // columns of a map (d threads) and every 256 / d-th share, and the shares' groups meet in LDS.
 template <typename T>
@@ -637,12 +783,13 @@ __global__ __launch_bounds__(256) void k_diff_join(DiffParams p) {
 // 1024 x 1024, 5 heads of 2 x 64 29 (40) / 23 (80) / 19; 3000 x 3000, 8 heads of 2 x 128 on 2 129 (188) / 168 / 248, 4 heads on 4 at 1511 70 (48) / 49 / 49.
 // Keys: shared out where the tiles leave the chip idle, at least 128 each.  us with 1 / 2 / 4 / 8 / .. shares: 64 tiles of 8192 keys 79 / 50 / 33 / 40 / 53; 16 tiles
 // 79 / 47 / 29 / 21 / 19 / 28; 80 tiles of 2048 keys 26 / 24 / 30; 160 tiles of 1024 keys 19 / 33: the sums' way through memory costs more than it brings.
-struct DiffPlan { int rows_a_tile, tiles, splits; };
-static DiffPlan diff_plan(int dtype, long long bh, int rows, int lk) {
+struct DiffPlan { bool keys_in_lds; int rows_a_tile, tiles, splits; };
+static DiffPlan diff_plan(int dtype, long long bh, int rows, int lk, int d) {
   DiffPlan a{};
-  a.rows_a_tile = dtype == AD_F32 ? 16 : bh * ((rows + 127) / 128) >= 150 ? 128 : bh * ((rows + 63) / 64) >= 150 ? 64 : 32;
+  a.keys_in_lds = dtype == AD_BF16 && lk <= 96 && d <= 64;
+  a.rows_a_tile = dtype == AD_F32 ? 16 : a.keys_in_lds ? 128 : bh * ((rows + 127) / 128) >= 150 ? 128 : bh * ((rows + 63) / 64) >= 150 ? 64 : 32;
   a.tiles = (rows + a.rows_a_tile - 1) / a.rows_a_tile;
-  const long long want = 256 / (bh * a.tiles), most = (lk + 127) / 128;
+  const long long want = 256 / (bh * a.tiles), most = a.keys_in_lds ? 1 : (lk + 127) / 128;
   a.splits = (int)std::max(1LL, std::min(std::min(want, most), (long long)kDiffMaxSplits));
   return a;
 }
@@ -685,6 +832,18 @@ static ad_status run_diff_mfma(const DiffParams& p, const DiffPlan& plan, unsign
   return run_diff_waves<NC, 1, NC <= 4 ? 2 : 1, OCC_FEW>(p, blocks, s);
 }
 
+template <int NC, int NB>
+static ad_status run_diff_blocks(const DiffParams& p, unsigned blocks, hipStream_t s) {
+  static std::atomic<bool> attr_set{false};
+  return launch_diff(k_diff_short<NC, NB>, 256, 2 * NB * 32 * diff_pitch(NC) + 8 * p.d, attr_set, blocks, p, s);
+}
+template <int NC>
+static ad_status run_diff_short(const DiffParams& p, unsigned blocks, hipStream_t s) {
+  if (p.lk <= 32) return run_diff_blocks<NC, 1>(p, blocks, s);
+  if (p.lk <= 64) return run_diff_blocks<NC, 2>(p, blocks, s);
+  return run_diff_blocks<NC, 3>(p, blocks, s);
+}
+
 static ad_status run_diff(int dtype, DiffParams p, const DiffPlan& plan, int batch, hipStream_t s) {
   p.tiles = plan.tiles;
   p.splits = plan.splits;
@@ -695,7 +854,11 @@ static ad_status run_diff(int dtype, DiffParams p, const DiffPlan& plan, int bat
   const unsigned blocks = (unsigned)(batch * p.kv_heads) * (unsigned)p.tiles * (unsigned)p.splits;
   const int chunks = (p.d + 15) / 16;
   ad_status st;
-  if (dtype == AD_BF16) {
+  if (plan.keys_in_lds) {
+    if (chunks <= 2) st = run_diff_short<2>(p, blocks, s);
+    else if (chunks == 3) st = run_diff_short<3>(p, blocks, s);
+    else st = run_diff_short<4>(p, blocks, s);
+  } else if (dtype == AD_BF16) {
     if (chunks <= 2) st = run_diff_mfma<2>(p, plan, blocks, s);
     else if (chunks == 3) st = run_diff_mfma<3>(p, plan, blocks, s);
     else if (chunks == 4) st = run_diff_mfma<4>(p, plan, blocks, s);
@@ -725,7 +888,7 @@ extern "C" {
 size_t ad_diff_attention_workspace_bytes(int dtype, int batch, int l, int lk, int heads, int kv_heads, int head_dim) {
   if ((dtype != AD_BF16 && dtype != AD_F32) || !diff_shape_ok(batch, l, lk, heads, kv_heads, head_dim)) return 0;
   const long long rows = (long long)l * (heads / kv_heads), bh = (long long)batch * kv_heads;
-  return diff_partial_bytes(bh, rows, diff_plan(dtype, bh, (int)rows, lk).splits, head_dim);
+  return diff_partial_bytes(bh, rows, diff_plan(dtype, bh, (int)rows, lk, head_dim).splits, head_dim);
 }
 
 ad_status ad_diff_attention_forward(int dtype, const void* q, const void* k, const void* v, int batch, int l, int lk, int heads, int kv_heads,
@@ -757,7 +920,7 @@ ad_status ad_diff_attention_forward(int dtype, const void* q, const void* k, con
   p.div_group = make_fastdiv((unsigned)p.group);
   p.div_kv = make_fastdiv((unsigned)kv_heads);
   const long long bh = (long long)batch * kv_heads;
-  DiffPlan plan = diff_plan(dtype, bh, p.rows, lk);
+  DiffPlan plan = diff_plan(dtype, bh, p.rows, lk, head_dim);
   if (plan.splits > 1 && (!workspace || workspace_bytes < diff_partial_bytes(bh, p.rows, plan.splits, head_dim))) plan.splits = 1;
   ProfLaunch pl(dtype == AD_BF16 ? "diff_attn_bf16" : "diff_attn_f32", 12.0 * batch * heads * head_dim * l * lk,
                 2.0 * esize(dtype) * batch * head_dim * (2.0 * l * heads + 2.0 * lk * kv_heads), (hipStream_t)stream, batch * l, lk, (int)(heads * w));
