@@ -801,11 +801,17 @@ static size_t diff_partial_bytes(long long bh, long long rows, int splits, int d
   return splits > 1 ? (size_t)(bh * rows * splits) * (4 * (size_t)d + 4) * sizeof(float) : 0;
 }
 
+// lds_bytes: beyond 64 KiB a kernel has to be told, once on every device (attr_set: a bit for each of the first 64)
 template <typename K>
-static ad_status launch_diff(K kern, int threads, int lds_bytes, std::atomic<bool>& attr_set, unsigned blocks, const DiffParams& p, hipStream_t s) {
-  if (lds_bytes > 65536 && !attr_set) {
-    AD_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
-    attr_set = true;
+static ad_status launch_diff(K kern, int threads, int lds_bytes, std::atomic<unsigned long long>& attr_set, unsigned blocks, const DiffParams& p, hipStream_t s) {
+  if (lds_bytes > 65536) {
+    int device = 0;
+    AD_HIP(hipGetDevice(&device));
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (!(attr_set & bit)) {
+      AD_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
+      attr_set |= bit;
+    }
   }
   hipLaunchKernelGGL(kern, dim3(blocks), dim3(threads), lds_bytes, s, p);
   AD_HIP(hipGetLastError());
@@ -814,13 +820,13 @@ static ad_status launch_diff(K kern, int threads, int lds_bytes, std::atomic<boo
 
 template <int DT>
 static ad_status run_diff_f32(const DiffParams& p, unsigned blocks, hipStream_t s) {
-  static std::atomic<bool> attr_set{false};
+  static std::atomic<unsigned long long> attr_set{0};
   return launch_diff(k_diff_f32<DT>, 256, 4 * 16 * (64 * ((2 * DT + 3) / 4) + 4) * 4, attr_set, blocks, p, s);
 }
 
 template <int NC, int WR, int WB, int OCC>
 static ad_status run_diff_waves(const DiffParams& p, unsigned blocks, hipStream_t s) {
-  static std::atomic<bool> attr_set{false};
+  static std::atomic<unsigned long long> attr_set{0};
   return launch_diff(k_diff_mfma<NC, WR, WB, OCC>, 128 * WR * WB, 4 * 64 * WB * diff_pitch(NC) + 8 * p.d, attr_set, blocks, p, s);
 }
 // OCC: wavefronts per SIMD that the register budget is set for; heads wider than 96 have a CU's LDS for one workgroup
@@ -834,7 +840,7 @@ static ad_status run_diff_mfma(const DiffParams& p, const DiffPlan& plan, unsign
 
 template <int NC, int NB>
 static ad_status run_diff_blocks(const DiffParams& p, unsigned blocks, hipStream_t s) {
-  static std::atomic<bool> attr_set{false};
+  static std::atomic<unsigned long long> attr_set{0};
   return launch_diff(k_diff_short<NC, NB>, 256, 2 * NB * 32 * diff_pitch(NC) + 8 * p.d, attr_set, blocks, p, s);
 }
 template <int NC>
@@ -902,8 +908,8 @@ ad_status ad_diff_attention_forward(int dtype, const void* q, const void* k, con
   if (head_dim % vn) AD_FAIL(AD_ERR_INVALID, "differential attention: head_dim must be a multiple of %d", vn);
   const long long w = 2LL * head_dim;
   if (ldq < heads * w || ldk < kv_heads * w || ldv < kv_heads * w || ldo < heads * w) AD_FAIL(AD_ERR_INVALID, "differential attention: bad leading dimension");
-  // the tile loads address 64 keys through 32-bit byte offsets from the first of them
-  if (dtype == AD_BF16 && (ldk >= (1 << 24) || ldv >= (1 << 24))) AD_FAIL(AD_ERR_INVALID, "differential attention: rows of keys or values too far apart");
+  // the tile loads address up to 128 keys through 32-bit byte offsets from the first of them
+  if (dtype == AD_BF16 && (ldk > (1 << 23) - 256 || ldv > (1 << 23) - 256)) AD_FAIL(AD_ERR_INVALID, "differential attention: rows of keys or values too far apart");
   if ((ldq | ldk | ldv | ldo) % vn || (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15))
     AD_FAIL(AD_ERR_INVALID, "differential attention: tensors and rows must be aligned to 16 bytes");
   if (((uintptr_t)key_lens | (uintptr_t)lambda | (uintptr_t)norm_gain) % 4 || (uintptr_t)workspace % 16) AD_FAIL(AD_ERR_INVALID, "differential attention: misaligned argument");

@@ -3,8 +3,9 @@
 Tolerances, element by element, from the roundings (u = 2^-24).  A score is a sum of d products held in fp32: off by at most (d + 4) u sum |q||k| / sqrt d, d the
 term that covers every order of summation; the exponential's argument is that score times log2 e less a reference, off by 3 u of their sizes more, and the
 exponential by 2 u.  With e the largest of these over a row's keys, a map's weights are off by a factor within 1 +- 2 e (numerator and denominator), its sums by the number of
-terms that follow each other in one register, at most 16 + lk / 16 times u.  bf16 rounds each weight, once: finfo(bf16).eps / 2 of itself.  So a map's row is off by
-(2 e + (lk / 16 + 24) u [+ 2^-8]) sum p |v|, the difference by the first map's plus |lambda| times the second's, and the result by half a step of its type more.
+terms that follow each other in one register, at most 16 + lk / 16 times u.  bf16 rounds each weight, once: finfo(bf16).eps / 2 of itself, 2^-8, and a
+sum of such weights is off by as much of itself at most, which moves the quotient by 2^-8 of the row.  So a map's row is off by
+(2 e + (lk / 16 + 24) u [+ 2^-8]) sum p |v| [+ 2^-8 |sum p v|], the difference by the first map's plus |lambda| times the second's, and the result by half a step of its type more.
 The norm divides by the row's root mean square: the relative error of that root is at most the norm of the row's errors over the norm of the row."""
 import numpy as np
 import pytest
@@ -50,6 +51,8 @@ def reference(dtype, q, k, v, lam, lens, causal, gain, eps, scale):
                 rel = e + (w * e).sum(-1, keepdims=True)
                 vv = np.abs(v[i, :n, g])
                 o += factor * (w @ v[i, :n, g])
+                if dtype == B.AD_BF16:
+                    err += abs(factor) * 2.0 ** -8 * np.abs(w @ v[i, :n, g])
                 err += abs(factor) * ((w * (rel + (lk / 16 + 24) * U + (2.0 ** -8 if dtype == B.AD_BF16 else 0.0))) @ vv)
             err += 6 * U * np.abs(o)
             if gain is not None:
@@ -177,6 +180,30 @@ def test_lengths_and_what_lies_behind_them(dtype, causal, l, lk, lens, d):
         if n <= 0:
             assert (got[i] == 0).all()
     c.check(work=False)
+
+
+# enough rows for tiles of 128 and of 64, every class of head width, keys that end inside a tile and beside one, a key more than lies in LDS at once
+@pytest.mark.parametrize("d", [16, 32, 48, 64, 80, 96, 128])
+@pytest.mark.parametrize("l,lk,causal", [(3900, 130, False), (3900, 320, True), (2000, 193, False), (2000, 64, True), (3900, 97, False), (3900, 96, False)])
+def test_tiles_of_many_rows(d, l, lk, causal):
+    Case(B.AD_BF16, 1, l, lk, 5, 5, d, causal=causal, lens=[lk - 1] if lk == 193 else None).check()
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_many_rows_that_share_keys(d):
+    """Rows of one tile are queries and heads: 3 queries x 3 heads, tiles that end inside a query."""
+    Case(B.AD_BF16, 2, 1001, 200, 9, 3, d, causal=True, lens=[200, 77]).check()
+
+
+@pytest.mark.parametrize("d,nan_at", [(32, 40), (64, 70), (32, 130), (128, 130)])
+def test_what_lies_behind_the_keys_of_a_tensor(d, nan_at):
+    """k and v are the front part of larger buffers whose next rows are NaN: nothing behind the last key is used."""
+    c = Case(B.AD_BF16, 1, 200, nan_at, 2, 2, d)
+    for name in ("k", "v"):
+        whole = torch.full((1, nan_at + 200, 4 * d), float("nan"), device=DEV, dtype=torch.bfloat16)
+        whole[:, :nan_at] = getattr(c, name)
+        setattr(c, name, whole[:, :nan_at])
+    c.check()
 
 
 @pytest.mark.parametrize("dtype", DT)
