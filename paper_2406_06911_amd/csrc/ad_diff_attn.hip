@@ -733,7 +733,7 @@ __global__ __launch_bounds__(256) void k_diff_join(DiffParams p) {
   // quad `quad` of a record's 4 d sums, shares first, first + groups, ...; what is read first does not need the factors
   const int groups = 256 / d, quad = tid % d, first = tid / d;
   const bool on = first < groups;
-  constexpr int UN = 4;
+  constexpr int UN = 16;                        // in flight: all 64 shares of a head of 2 x 64 (one token x 8190, 32 rows: 12.8 us, with four in flight 13.7)
   f32x4 x[UN];
   auto fetch = [&](int s0) {
 #pragma unroll
