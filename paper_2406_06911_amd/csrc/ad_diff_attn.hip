@@ -312,21 +312,32 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
   const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds + wave * 1024u;
   struct Stream { const bf16* at; int left; };                 // the next tile, and the keys from its first on
   Stream next_k{kbase + (size_t)from * p.ldk, len - from}, next_v{vbase + (size_t)from * p.ldv, len - from};
-  auto issue = [&](Stream& n, int ld, unsigned at, auto swizzle) __attribute__((always_inline)) {
-    u32x4 rsrc = make_rsrc_words(n.at, (unsigned)((min(n.left, KEYS) - 1) * ld + w) * 2u);
+  // descriptor of the next tile; behind the last one nothing lies in range
+  auto next_tile = [&](Stream& n, int ld) __attribute__((always_inline)) {
+    u32x4 rsrc = make_rsrc_words(n.at, n.left > 0 ? (unsigned)((min(n.left, KEYS) - 1) * ld + w) * 2u : 0u);
 #pragma unroll
     for (int e = 0; e < 4; ++e) rsrc[e] = __builtin_amdgcn_readfirstlane(rsrc[e]);     // a descriptor lies in scalar registers
-#pragma unroll
-    for (int x = 0; x < LPT; ++x) {
-      const int id = (x * NW + wave) * 64 + lane, r = id / CPR, c = (id % CPR) ^ swizzle(r);
-      dma_load16(rsrc, c * 8 < w ? (unsigned)(r * ld) * 2u + c * 16u : kOob, 0u, at + x * NW * 1024u);
-    }
     n.at += (size_t)KEYS * ld;
     n.left -= KEYS;
+    return rsrc;
   };
-  auto issue_k = [&](int slot) { issue(next_k, p.ldk, lds_base + slot * TILE, [](int r) { return PITCH == 128 ? (r >> 1) & 7 : r & 15; }); };
-  auto issue_v = [&](int slot) { issue(next_v, p.ldv, lds_base + (2 + slot) * TILE, [](int r) { return PITCH == 128 ? (r << 1) & 4 : (r & 3) << 2; }); };
-  if (ntiles > 0) { issue_k(0); issue_v(0); }
+  auto piece = [&](const u32x4& rsrc, int ld, unsigned at, int x, auto swizzle) __attribute__((always_inline)) {
+    const int id = (x * NW + wave) * 64 + lane, r = id / CPR, c = (id % CPR) ^ swizzle(r);
+    dma_load16(rsrc, c * 8 < w ? (unsigned)(r * ld) * 2u + c * 16u : kOob, 0u, at + x * NW * 1024u);
+  };
+  auto piece_k = [&](const u32x4& rsrc, int slot, int x) __attribute__((always_inline)) {
+    piece(rsrc, p.ldk, lds_base + slot * TILE, x, [](int r) { return PITCH == 128 ? (r >> 1) & 7 : r & 15; });
+  };
+  auto piece_v = [&](const u32x4& rsrc, int slot, int x) __attribute__((always_inline)) {
+    piece(rsrc, p.ldv, lds_base + (2 + slot) * TILE, x, [](int r) { return PITCH == 128 ? (r << 1) & 4 : (r & 3) << 2; });
+  };
+  if (ntiles > 0) {
+    const u32x4 rk = next_tile(next_k, p.ldk), rv = next_tile(next_v, p.ldv);
+#pragma unroll
+    for (int x = 0; x < LPT; ++x) piece_k(rk, 0, x);
+#pragma unroll
+    for (int x = 0; x < LPT; ++x) piece_v(rv, 0, x);
+  }
 
   // what the end needs is asked for now: the gains go behind the tiles, a wavefront of the second map keeps lambda
   float* const gains = (float*)(lds + 4 * TILE);
@@ -383,9 +394,10 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
     return __builtin_amdgcn_fdot2_f32_bf16(e, ones, sum, false);
   };
   // A step, in one straight line: the scores of the next block, the products of the block before with its values, and between those MFMAs the weights of
-  // this block, x its place in its tile.  Fragments are asked for AHEAD MFMAs early.
-  auto step = [&](int x) __attribute__((always_inline)) {
-    constexpr int NM = 3 * NC, AHEAD = 3;
+  // this block, x its place in its tile, and what else goes beside MFMA g.  Fragments are asked for AHEAD MFMAs early.
+  constexpr int NM = 3 * NC;
+  auto step = [&](int x, auto&& beside) __attribute__((always_inline)) {
+    constexpr int AHEAD = 3;
     bf16x8 fr[AHEAD + 1];
     auto fetch = [&](int g) { fr[g % (AHEAD + 1)] = g < NC ? k_frag(1 - x, g) : v_frag(1 - x, g - NC); };
 #pragma unroll
@@ -401,6 +413,7 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
       const bf16x8& f = fr[g % (AHEAD + 1)];
       if constexpr (g < NC) s[1 - x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[g], s[1 - x], 0, 0, 0);
       else o[(g - NC) >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[1 - x][(g - NC) & 1], o[(g - NC) >> 1], 0, 0, 0);
+      beside(g_);
       __builtin_amdgcn_sched_barrier(0);
     });
     return sum[0] + sum[1];
@@ -448,7 +461,11 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
     for (int at = tid * 16; at < TILE; at += 16 * 64 * NW) *(f32x4*)(lds + 3 * TILE + at) = f32x4{0.f, 0.f, 0.f, 0.f};
     wait_vmcnt<0>();
     __syncthreads();
-    if (ntiles > 1) issue_k(1);
+    {
+      const u32x4 rk = next_tile(next_k, p.ldk);
+#pragma unroll
+      for (int x = 0; x < LPT; ++x) piece_k(rk, 1, x);
+    }
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
 #pragma unroll
@@ -458,7 +475,7 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
 #pragma unroll 1
     for (int t = 0; t < ntiles; ++t) {
       mask(t, 0);
-      settle(0, step(0));                                      // k: tile t, v: tile t - 1
+      settle(0, step(0, [](auto) {}));                                   // k: tile t, v: tile t - 1
 #pragma unroll
       for (int c = 0; c < NC; ++c) k_at[c] ^= TILE;
 #pragma unroll
@@ -466,15 +483,24 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
       // tile t + 1 of k and tile t of v have landed, and everybody is done with tile t of k and tile t - 1 of v
       wait_vmcnt<0>();
       __syncthreads();
-      if (t + 2 < ntiles) issue_k(t & 1);
-      if (t + 1 < ntiles) issue_v((t + 1) & 1);
+      const u32x4 rk = next_tile(next_k, p.ldk), rv = next_tile(next_v, p.ldv);
       mask(t, 1);
-      settle(1, step(1));                                      // k: tile t + 1 (behind the last tile: whatever lies there, not used), v: tile t
+      // k: tile t + 1 (behind the last tile: zeros, not used), v: tile t.  The loads of k's tile t + 2 and v's t + 1 are spread over the step: all at once they
+      // fill the load unit's queue, and the wavefront waits
+      settle(1, step(1, [&](auto g_) __attribute__((always_inline)) {
+        constexpr int g = decltype(g_)::value, N = 2 * LPT;
+#pragma unroll
+        for (int x = N * g / NM; x < N * (g + 1) / NM; ++x) {
+          if (x < LPT) piece_k(rk, t & 1, x);
+          else piece_v(rv, (t + 1) & 1, x - LPT);
+        }
+      }));
     }
 #pragma unroll
     for (int n = 0; n < 2 * NC; ++n) o[n >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(1, n), pb[1][n & 1], o[n >> 1], 0, 0, 0);
   }
 
+  wait_vmcnt<0>();                                             // the last tiles' loads write LDS too
   l_run += other_half(l_run, low);
   // sums change hands in LDS, four registers of all lanes at a time
   auto quad = [&](int t, int q4) { return f32x4{o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]}; };
