@@ -267,11 +267,14 @@ __global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p)
 // block between them; the order is pinned, left alone the exponentials gather behind the MFMAs.  So k runs a tile ahead of v, and a barrier every two steps is enough.
 //
 // Probabilities are rounded to bf16 for the product with v, and the row's sum is of the rounded ones (half the instructions of a sum in front of the
-// rounding; the weights then add up to 1); scores, sums and references are fp32; q is not scaled in front of the product (a rounding less).
+// rounding; the weights then add up to 1); scores, sums and references are fp32; q is not scaled in front of the product (a rounding less).  The difference of the maps
+// is smaller than the maps, so those roundings would leave a result 1.53 to 1.55 times as far off as one that is only rounded at the end (relative L2, scores of
+// variance 1); the first 16 of every 64 keys go into the product in two parts, the second what the rounding dropped, which share their fragments of v: 1.43 times, for 11 to 13 % of the
+// time (all keys in two parts: for twice the products with v).
 //
-// Bound: narrow heads by vector instructions (55 a step beside 6 MFMAs at d = 32), wide ones by the MFMAs, of which 12 d of the 12 d + exponentials operations
-// are counted; at 9216 x 9216 the clock falls to 1.9 GHz.  us: 2 x 9216 x 9216, 5 heads of 2 x 32 375 (870 TFLOP/s), 2 x 2304 x 2304, 5 of 2 x 64 53 (775; 180
-// workgroups on 256 CUs), 1511 x 6007 causal, 8 of 2 x 128 on 2 152 (640; 190 workgroups), one token x 8190 14.
+// Bound: narrow heads by vector instructions (about 60 a step beside 7 MFMAs at d = 32), wide ones by the MFMAs (19 to 22 ns each on random numbers, 17 on constants); at 9216 x 9216
+// the clock falls to 1.9 GHz.  us: 2 x 9216 x 9216, 5 heads of 2 x 32 414 (790 TFLOP/s at 12 d operations a pair), 2 x 2304 x 2304, 5 of 2 x 64 56 (725; 180 workgroups on
+// 256 CUs), 1511 x 6007 causal, 8 of 2 x 128 on 2 153 (637; 190 workgroups), one token x 8190 13.5.
 // =================================================================================================
 // f(0), f(1), .. f(N - 1) with constants: a loop of this length is not unrolled by itself, and arrays indexed in it would go to memory
 template <int N, typename F> __device__ __forceinline__ void unrolled(F&& f) {
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
     if (16 * c + 8 * half < d) qf[c] = *(const bf16x8*)(qrow + 16 * c + 8 * half);
   }
   f32x16 o[NC], s[2];
-  bf16x8 pb[2][2];
+  bf16x8 pb[2][2], dropped;                                    // weights; what the rounding of a tile's first 16 dropped
   float m_ref = -INFINITY, neg = __builtin_nanf(""), l_run = 0.f;
 #pragma unroll
   for (int t = 0; t < NC; ++t)
@@ -388,9 +391,14 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
   const bf16x2 ones = {(bf16)1.f, (bf16)1.f};
   // weights from registers r and r + 1 of the scores; returns the row's sum with them
   auto weigh = [&](int x, int r, float sum) __attribute__((always_inline)) {
-    const bf16x2 e = {(bf16)__builtin_amdgcn_exp2f(fmaf(s[x][r], p.scale_log2, neg)), (bf16)__builtin_amdgcn_exp2f(fmaf(s[x][r + 1], p.scale_log2, neg))};
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[x][r], p.scale_log2, neg)), e1 = __builtin_amdgcn_exp2f(fmaf(s[x][r + 1], p.scale_log2, neg));
+    const bf16x2 e = {(bf16)e0, (bf16)e1};
     pb[x][r >> 3][r & 7] = e[0];
     pb[x][r >> 3][(r & 7) + 1] = e[1];
+    if (x == 0 && r < 8) {
+      dropped[r] = (bf16)(e0 - (float)e[0]);
+      dropped[r + 1] = (bf16)(e1 - (float)e[1]);
+    }
     return __builtin_amdgcn_fdot2_f32_bf16(e, ones, sum, false);
   };
   // A step, in one straight line: the scores of the next block, the products of the block before with its values, and between those MFMAs the weights of
@@ -413,6 +421,8 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
       const bf16x8& f = fr[g % (AHEAD + 1)];
       if constexpr (g < NC) s[1 - x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[g], s[1 - x], 0, 0, 0);
       else o[(g - NC) >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[1 - x][(g - NC) & 1], o[(g - NC) >> 1], 0, 0, 0);
+      if constexpr (g >= NC && (g - NC) % 2 == 0)
+        if (x == 1) o[(g - NC) >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, dropped, o[(g - NC) >> 1], 0, 0, 0);
       beside(g_);
       __builtin_amdgcn_sched_barrier(0);
     });
