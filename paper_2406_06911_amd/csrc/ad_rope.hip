@@ -25,7 +25,7 @@ constexpr int kRopeMaxDim = 128;   // widest head: the limit of the attention ke
 // read them from there.  A head is shared out over a power of two of lanes, each with two accesses of VN elements (up to 16 bytes each): the two sides of VN
 // pairs where the pairs lie half the rotated part apart, VN pairs in a row where they are neighbours; the part that is not rotated lies behind.  The norm's
 // sums go over those lanes.  Bound by memory: every element is read once and written once; a lane writes where it has read, so q_out may be q.
-// us: rotation of 16384 rows of 20 heads of 64, bf16, 84 MB 15.1 (5.6 TB/s), 10006 of 10 heads of 80, fp32, 64 MB 11.8 (5.4); norm and rotation of 18432 rows of
+// us: rotation of 16384 rows of 20 heads of 64, bf16, 84 MB 15.1 to 18.4 from run to run (5.6 to 4.6 TB/s), 10006 of 10 heads of 80, fp32, 64 MB 11.8 (5.4); norm and rotation of 18432 rows of
 // 20 heads of 32, bf16, 47 MB 11.4 (4.2).  With the angles in every group of lanes and the gains in registers 15.3, 12.3 and 14.4; two, three or six heads in flight and
 // occupancies of six and eight wavefronts: level or slower.
 // =================================================================================================
