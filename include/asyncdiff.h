@@ -397,7 +397,7 @@ ad_status ad_qk_norm_rope_forward(int dtype, int norm, const ad_rope_cfg* cfg, c
  *   out = out_scale * o * rsqrt(mean o^2 + norm_eps) * norm_gain  per head, or out_scale * o where norm_gain is NULL.
  *   q [batch][l][ldq], out [batch][l][ldo]: `heads` heads of 2 head_dim columns; k [batch][lk][ldk], v [batch][lk][ldv]: `kv_heads` heads, each shared by
  *   heads / kv_heads query heads that follow each other.  head_dim <= 128, a multiple of 8 (bf16) or 4 (fp32); tensors and rows 16-byte aligned.
- *   out must not overlap what is read.
+ *   out must not overlap what is read; bf16: ldk and ldv at most 2^23 - 256.
  *   key_lens   int32 [batch] or NULL: sample b has keys 0 .. key_lens[b] - 1 (held to 0 .. lk); what lies behind them does not matter, NaN included;
  *   causal     query i sees keys 0 .. i + len - l, len the sample's keys (the last query sees them all).  A key that only some rows of the call see
  *              takes part in the others with weight 0: its values must be finite there;

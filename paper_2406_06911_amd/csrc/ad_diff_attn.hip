@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256, DT <= 4 ? 2 : 1) void k_diff_f32(DiffParams p)
   const bool live = row < p.rows;
   const int i = live ? (int)fast_div((unsigned)row, p.div_group) : 0, hg = live ? row - i * p.group : 0;
   // keys that this lane's row sees: 0 .. limit - 1; the workgroup's are those of its last row
-  auto limit_of = [&](int query) { return p.causal ? min(max(query + len - p.l + 1, 0), len) : len; };
+  auto limit_of = [&](int query) { return p.causal ? min(max(query + (len - p.l + 1), 0), len) : len; };
   const int limit = live ? limit_of(i) : len, limit_first = limit_of((int)fast_div(tile * 16u, p.div_group));
   const int last = min((int)tile * 16 + 15, p.rows - 1);
   const int from = split * p.split_keys, to = min(from + p.split_keys, limit_of((int)fast_div((unsigned)last, p.div_group)));
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
   const int d = p.d, w = 2 * d;
   const int len = __builtin_amdgcn_readfirstlane(p.key_lens ? min(max(p.key_lens[b], 0), p.lk) : p.lk);
   auto limit_of = [&](int row) {
-    return p.causal ? min(max((int)fast_div((unsigned)min(row, p.rows - 1), p.div_group) + len - p.l + 1, 0), len) : len;
+    return p.causal ? min(max((int)fast_div((unsigned)min(row, p.rows - 1), p.div_group) + (len - p.l + 1), 0), len) : len;
   };
   const int row0 = tile * (32 * WR) + 32 * row_wave, row = row0 + l32;
   const int rowc = min(row, p.rows - 1);                       // rows behind the last repeat it, and are not stored
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(128 * WR * WB, OCC) void k_diff_mfma(DiffParams p) 
     });
     return sum[0] + sum[1];
   };
-  // first block of this wavefront (of 32 keys, two a tile) of which a row does not see all
+  // whether some row does not see all of block x of tile t
   auto masked = [&](int t, int x) { return from + KEYS * t + 64 * my_block + 32 * x + 32 > lim_first; };
   auto mask = [&](int t, int x) __attribute__((always_inline)) {
     if (masked(t, x)) {
@@ -628,7 +628,7 @@ __global__ __launch_bounds__(256, NC <= 2 ? 3 : 2) void k_diff_short(DiffParams 
   const int len = __builtin_amdgcn_readfirstlane(p.key_lens ? min(max(p.key_lens[b], 0), p.lk) : p.lk);
   const int row = tile * 128 + wave * 32 + l32, rowc = min(row, p.rows - 1);
   const int i = (int)fast_div((unsigned)rowc, p.div_group), head = hk * p.group + rowc - i * p.group;
-  auto limit_of = [&](int query) { return p.causal ? min(max(query + len - p.l + 1, 0), len) : len; };
+  auto limit_of = [&](int query) { return p.causal ? min(max(query + (len - p.l + 1), 0), len) : len; };
   const int limit = limit_of(i), lim_first = limit_of((int)fast_div((unsigned)min((int)tile * 128 + wave * 32, p.rows - 1), p.div_group));
 
   const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds + wave * 1024u;
@@ -830,7 +830,7 @@ static DiffPlan diff_plan(int dtype, long long bh, int rows, int lk, int d) {
   return a;
 }
 static bool diff_shape_ok(int batch, int l, int lk, int heads, int kv_heads, int d) {
-  return batch >= 1 && l >= 1 && lk >= 1 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 1 && d <= 128 &&
+  return batch >= 1 && l >= 1 && lk >= 1 && lk <= 0x7fff0000 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 1 && d <= 128 &&
          (long long)l * (heads / kv_heads) <= 0x7fffff00LL && (long long)batch * kv_heads * ((long long)l * (heads / kv_heads) / 16 + 1) <= 0x1ffffffLL;
 }
 static size_t diff_partial_bytes(long long bh, long long rows, int splits, int d) {

@@ -109,7 +109,7 @@ GOOD_DIFF = dict(dtype=B.AD_BF16, q=FAKE, k=2 * FAKE, v=3 * FAKE, b=2, l=8, lk=1
 @pytest.mark.parametrize("change", [dict(dtype=2), dict(q=None), dict(k=None), dict(v=None), dict(lam=None), dict(out=None), dict(b=0), dict(l=0), dict(lk=0), dict(lk=-5), dict(heads=0), dict(kv=0),
                                     dict(heads=5), dict(d=0), dict(d=60), dict(d=136, ldq=2000, ldk=2000, ldv=2000, ldo=2000), dict(dtype=B.AD_F32, d=6), dict(ldq=504), dict(ldk=248),
                                     dict(ldv=248), dict(ldo=504), dict(ldq=514), dict(ldk=260), dict(q=FAKE + 8), dict(v=FAKE + 2), dict(out=FAKE + 4), dict(lens=FAKE + 1), dict(lam=FAKE + 2),
-                                    dict(gain=FAKE + 2), dict(ws=FAKE + 8), dict(eps=0.0), dict(eps=float("nan")), dict(scale=float("inf")), dict(b=1 << 20, l=1 << 20), dict(ldk=1 << 23), dict(ldv=1 << 24)], ids=str)
+                                    dict(gain=FAKE + 2), dict(ws=FAKE + 8), dict(eps=0.0), dict(eps=float("nan")), dict(scale=float("inf")), dict(b=1 << 20, l=1 << 20), dict(ldk=1 << 23), dict(ldv=1 << 24), dict(lk=0x7fff8000)], ids=str)
 def test_differential_attention_refuses(change):
     a = {**GOOD_DIFF, **change}
     st = L.ad_diff_attention_forward(a["dtype"], a["q"], a["k"], a["v"], a["b"], a["l"], a["lk"], a["heads"], a["kv"], a["d"], a["ldq"], a["ldk"], a["ldv"], a["ldo"], a["lens"], a["causal"],
