@@ -817,13 +817,16 @@ __global__ __launch_bounds__(256) void k_diff_join(DiffParams p) {
 // Rows, bf16: the largest tile that gives 150 workgroups.  A larger tile reads keys and values less often, and its wavefronts hide each other's waits; too few
 // leave CUs idle.  us at 128 / 64 / 32 rows: 2304 x 2304, 5 heads of 2 x 64, two samples 54 (180 workgroups) / 58 / 86, one sample 52 (90) / 41 / 57;
 // 1024 x 1024, 5 heads of 2 x 64 29 (40) / 23 (80) / 19; 3000 x 3000, 8 heads of 2 x 128 on 2 129 (188) / 168 / 248, 4 heads on 4 at 1511 70 (48) / 49 / 49.
+// 257 to 384 workgroups of 128 rows give some CUs two and most one, where 64 rows even out: 280 of 2 x 32 / 2 x 64 105 -> 88 / 175 -> 154, 320 of 2 x 32 / 64 / 128 122 -> 104 /
+// 204 -> 182 / 417 -> 337; not 500 (206 / 224, 337 / 358), 720 (425 / 456) or 180 (44 / 47).
 // Keys: shared out where the tiles leave the chip idle, at least 128 each.  us with 1 / 2 / 4 / 8 / .. shares: 64 tiles of 8192 keys 79 / 50 / 33 / 40 / 53; 16 tiles
 // 79 / 47 / 29 / 21 / 19 / 28; 80 tiles of 2048 keys 26 / 24 / 30; 160 tiles of 1024 keys 19 / 33: the sums' way through memory costs more than it brings.
 struct DiffPlan { bool keys_in_lds; int rows_a_tile, tiles, splits; };
 static DiffPlan diff_plan(int dtype, long long bh, int rows, int lk, int d) {
   DiffPlan a{};
   a.keys_in_lds = dtype == AD_BF16 && lk <= 96 && d <= 64;
-  a.rows_a_tile = dtype == AD_F32 ? 16 : a.keys_in_lds ? 128 : bh * ((rows + 127) / 128) >= 150 ? 128 : bh * ((rows + 63) / 64) >= 150 ? 64 : 32;
+  const long long large = bh * ((rows + 127) / 128);
+  a.rows_a_tile = dtype == AD_F32 ? 16 : a.keys_in_lds ? 128 : large >= 150 && (large <= 256 || large > 384) ? 128 : bh * ((rows + 63) / 64) >= 150 ? 64 : 32;
   a.tiles = (rows + a.rows_a_tile - 1) / a.rows_a_tile;
   const long long want = 256 / (bh * a.tiles), most = a.keys_in_lds ? 1 : (lk + 127) / 128;
   a.splits = (int)std::max(1LL, std::min(std::min(want, most), (long long)kDiffMaxSplits));
@@ -868,7 +871,7 @@ static ad_status run_diff_waves(const DiffParams& p, unsigned blocks, hipStream_
 // OCC: wavefronts per SIMD that the register budget is set for; heads wider than 96 have a CU's LDS for one workgroup
 template <int NC>
 static ad_status run_diff_mfma(const DiffParams& p, const DiffPlan& plan, unsigned blocks, hipStream_t s) {
-  constexpr int OCC = NC <= 2 ? 4 : 2, OCC_FEW = NC > 6 ? 1 : OCC;
+  constexpr int OCC = NC <= 2 ? 4 : 2, OCC_FEW = NC > 6 ? 1 : NC <= 2 ? 3 : 2;
   if (plan.rows_a_tile == 128) return run_diff_waves<NC, 4, 1, OCC>(p, blocks, s);
   if (plan.rows_a_tile == 64) return run_diff_waves<NC, 2, 1, OCC_FEW>(p, blocks, s);
   return run_diff_waves<NC, 1, NC <= 4 ? 2 : 1, OCC_FEW>(p, blocks, s);

@@ -184,7 +184,7 @@ def test_lengths_and_what_lies_behind_them(dtype, causal, l, lk, lens, d):
 
 # enough rows for tiles of 128 and of 64, every class of head width, keys that end inside a tile and beside one, a key more than lies in LDS at once
 @pytest.mark.parametrize("d", [16, 32, 48, 64, 80, 96, 128])
-@pytest.mark.parametrize("l,lk,causal", [(3900, 130, False), (3900, 320, True), (2000, 193, False), (2000, 64, True), (3900, 97, False), (3900, 96, False)])
+@pytest.mark.parametrize("l,lk,causal", [(3900, 130, False), (3900, 320, True), (2000, 193, False), (2000, 64, True), (3900, 97, False), (3900, 96, False), (6700, 130, False)])
 def test_tiles_of_many_rows(d, l, lk, causal):
     Case(B.AD_BF16, 1, l, lk, 5, 5, d, causal=causal, lens=[lk - 1] if lk == 193 else None).check()
 
